@@ -499,6 +499,8 @@ falqon_status falqon_swiglu_bwd(const void* dh, int64_t ld_dh, const void* g, co
  *   labels    in   int64 [T]
  *   logp, lse out  fp32 [T]
  *   dlogits   out  [T, V] of dtype lt, row stride ld_d; it may be the logits themselves
+ *   lse_low   out, then in  fp32 [T], nullable: what rounding takes from lse.  logp does not depend on it.  Without it a backward call forms
+ *             exp(x - lse) from the rounded lse where |lse| < 64 (off by at most 2^-19 of itself), and the rows beyond are read twice
  * ws: falqon_logprob_workspace_bytes(T, V, P) bytes; P is that of falqon_preference_loss (1 where only this call uses it).
  */
 size_t falqon_logprob_workspace_bytes(int64_t T, int64_t V, int64_t P);   /* 0 if a size is invalid */
@@ -506,6 +508,11 @@ falqon_status falqon_token_logprob(const void* logits, falqon_dtype lt, int64_t 
                                    float* logp, float* lse, void* ws, size_t ws_bytes, void* stream);
 falqon_status falqon_token_logprob_bwd(const float* d_logp, const void* logits, falqon_dtype lt, int64_t T, int64_t V, int64_t ld,
                                        const int64_t* labels, const float* lse, void* dlogits, int64_t ld_d, void* stream);
+/* the same with lse_low, NULL in the calls above */
+falqon_status falqon_token_logprob_low(const void* logits, falqon_dtype lt, int64_t T, int64_t V, int64_t ld, const int64_t* labels,
+                                       float* logp, float* lse, float* lse_low, void* ws, size_t ws_bytes, void* stream);
+falqon_status falqon_token_logprob_bwd_low(const float* d_logp, const void* logits, falqon_dtype lt, int64_t T, int64_t V, int64_t ld,
+                                           const int64_t* labels, const float* lse, const float* lse_low, void* dlogits, int64_t ld_d, void* stream);
 
 /*
  * Paired preference loss and its gradient by every log-probability.  The tokens [offsets[i], offsets[i + 1]) are sequence i; sequences

@@ -382,14 +382,14 @@ def logprob_workspace_bytes(T: int, V: int, P: int = 1) -> int:
     return int(lib().falqon_logprob_workspace_bytes(T, V, P))
 
 
-def token_logprob(logits, labels, logp, lse, ws) -> None:
-    """logp = log softmax(logits)[label] and lse of every row; a label outside the vocabulary does not count (0 and 0)."""
-    _check(_native().token_logprob(logits, labels, logp, lse, ws, _stream()), "falqon_token_logprob")
+def token_logprob(logits, labels, logp, lse, ws, lse_low=None) -> None:
+    """logp = log softmax(logits)[label] and lse of every row; a label outside the vocabulary does not count (0 and 0).  lse_low: what rounding takes from lse."""
+    _check(_native().token_logprob(logits, labels, logp, lse, ws, lse_low, _stream()), "falqon_token_logprob")
 
 
-def token_logprob_bwd(d_logp, logits, labels, lse, dlogits) -> None:
-    """dlogits = d_logp (onehot(label) - softmax(logits)); dlogits may be the logits."""
-    _check(_native().token_logprob_bwd(d_logp, logits, labels, lse, dlogits, _stream()), "falqon_token_logprob_bwd")
+def token_logprob_bwd(d_logp, logits, labels, lse, dlogits, lse_low=None) -> None:
+    """dlogits = d_logp (onehot(label) - softmax(logits)); dlogits may be the logits.  Without lse_low, rows of |lse| >= 64 are read twice."""
+    _check(_native().token_logprob_bwd(d_logp, logits, labels, lse, dlogits, lse_low, _stream()), "falqon_token_logprob_bwd")
 
 
 def preference_loss(logp, ref_logp, offsets, loss, rewards, d_logp, ws, beta: float = 0.1, smoothing: float = 0.0) -> None:

@@ -125,18 +125,18 @@ class _TokenLogprobFn(torch.autograd.Function):
         x = logits.reshape(-1, logits.shape[-1])
         x = x if x.shape[1] == 1 or x.stride(1) == 1 else x.contiguous()
         T, V = x.shape
-        logp, lse = (torch.empty(T, dtype=torch.float32, device=x.device) for _ in range(2))
+        logp, lse, low = (torch.empty(T, dtype=torch.float32, device=x.device) for _ in range(3))
         l2 = labels.reshape(-1).contiguous()
-        _b.token_logprob(x, l2, logp, lse, torch.empty(_b.logprob_workspace_bytes(T, V), dtype=_U8, device=x.device))
-        ctx.save_for_backward(x, l2, lse)
+        _b.token_logprob(x, l2, logp, lse, torch.empty(_b.logprob_workspace_bytes(T, V), dtype=_U8, device=x.device), lse_low=low)
+        ctx.save_for_backward(x, l2, lse, low)
         ctx.shape = logits.shape
         return logp.reshape(labels.shape)
 
     @staticmethod
     def backward(ctx, d_logp):
-        x, labels, lse = ctx.saved_tensors
+        x, labels, lse, low = ctx.saved_tensors
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        _b.token_logprob_bwd(d_logp.reshape(-1).contiguous(), x, labels, lse, dx)
+        _b.token_logprob_bwd(d_logp.reshape(-1).contiguous(), x, labels, lse, dx, lse_low=low)
         return dx.reshape(ctx.shape), None
 
 

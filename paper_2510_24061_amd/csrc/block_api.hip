@@ -150,22 +150,34 @@ size_t falqon_logprob_workspace_bytes(int64_t T, int64_t V, int64_t P)
 falqon_status falqon_token_logprob(const void* logits, falqon_dtype lt, int64_t T, int64_t V, int64_t ld, const int64_t* labels,
                                    float* logp, float* lse, void* ws, size_t ws_bytes, void* stream)
 {
+    return falqon_token_logprob_low(logits, lt, T, V, ld, labels, logp, lse, nullptr, ws, ws_bytes, stream);
+}
+
+falqon_status falqon_token_logprob_low(const void* logits, falqon_dtype lt, int64_t T, int64_t V, int64_t ld, const int64_t* labels,
+                                       float* logp, float* lse, float* lse_low, void* ws, size_t ws_bytes, void* stream)
+{
     if (bad_type(lt)) return FALQON_ERR_ENUM;
     if (bad_logits(T, V) || ld < V) return FALQON_ERR_SHAPE;
     if (!logits || !labels || !logp || !lse) return FALQON_ERR_NULL;
-    if (any_odd(lt == FALQON_F32 ? 4 : 2, logits) || any_odd(8, labels) || any_odd(4, logp, lse) || any_misaligned(ws)) return FALQON_ERR_ALIGN;
+    if (any_odd(lt == FALQON_F32 ? 4 : 2, logits) || any_odd(8, labels) || any_odd(4, logp, lse, lse_low) || any_misaligned(ws)) return FALQON_ERR_ALIGN;
     if (!ws || ws_bytes < falqon_logprob_workspace_bytes(T, V, 1)) return FALQON_ERR_WORKSPACE;
-    return status_of(launch_token_logprob(TokenLogprob{logits, ld, labels, T, V, logp, lse, static_cast<float2*>(ws)}, lt == FALQON_F32, on(stream)));
+    return status_of(launch_token_logprob(TokenLogprob{logits, ld, labels, T, V, logp, lse, lse_low, static_cast<float2*>(ws)}, lt == FALQON_F32, on(stream)));
 }
 
 falqon_status falqon_token_logprob_bwd(const float* d_logp, const void* logits, falqon_dtype lt, int64_t T, int64_t V, int64_t ld,
                                        const int64_t* labels, const float* lse, void* dlogits, int64_t ld_d, void* stream)
 {
+    return falqon_token_logprob_bwd_low(d_logp, logits, lt, T, V, ld, labels, lse, nullptr, dlogits, ld_d, stream);
+}
+
+falqon_status falqon_token_logprob_bwd_low(const float* d_logp, const void* logits, falqon_dtype lt, int64_t T, int64_t V, int64_t ld,
+                                           const int64_t* labels, const float* lse, const float* lse_low, void* dlogits, int64_t ld_d, void* stream)
+{
     if (bad_type(lt)) return FALQON_ERR_ENUM;
     if (bad_logits(T, V) || ld < V || ld_d < V || (logits == dlogits && ld != ld_d)) return FALQON_ERR_SHAPE;
     if (!d_logp || !logits || !labels || !lse || !dlogits) return FALQON_ERR_NULL;
-    if (any_odd(lt == FALQON_F32 ? 4 : 2, logits, dlogits) || any_odd(8, labels) || any_odd(4, d_logp, lse)) return FALQON_ERR_ALIGN;
-    return status_of(launch_token_logprob_bwd(TokenLogprobBwd{d_logp, logits, ld, labels, lse, T, V, dlogits, ld_d}, lt == FALQON_F32, on(stream)));
+    if (any_odd(lt == FALQON_F32 ? 4 : 2, logits, dlogits) || any_odd(8, labels) || any_odd(4, d_logp, lse, lse_low)) return FALQON_ERR_ALIGN;
+    return status_of(launch_token_logprob_bwd(TokenLogprobBwd{d_logp, logits, ld, labels, lse, lse_low, T, V, dlogits, ld_d}, lt == FALQON_F32, on(stream)));
 }
 
 falqon_status falqon_preference_loss(const float* logp, const float* ref_logp, const int64_t* offsets, int64_t T, int64_t P, double beta,

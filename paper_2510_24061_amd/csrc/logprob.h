@@ -10,7 +10,7 @@ struct TokenLogprob {
     const void* logits; int64_t ld;
     const int64_t* labels;
     int64_t T, V;
-    float *logp, *lse;
+    float *logp, *lse, *lse_low;                 // lse_low may be null
     float2* partial;
 };
 hipError_t launch_token_logprob(const TokenLogprob& a, bool f32, hipStream_t stream);
@@ -19,7 +19,7 @@ struct TokenLogprobBwd {
     const float* d_logp;
     const void* logits; int64_t ld;
     const int64_t* labels;
-    const float* lse;
+    const float *lse, *lse_low;
     int64_t T, V;
     void* out; int64_t ld_out;
 };

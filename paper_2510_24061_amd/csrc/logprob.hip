@@ -5,6 +5,11 @@
 //   loss = mean_p (1 - eps) softplus(-z_p) + eps softplus(z_p);   d loss / d logp_t = -+ beta / P ((1 - eps) sigma(-z) - eps sigma(z))
 //   dx_tv = d_t ([v = label] - exp(x_tv - lse_t)),  0 for tokens that do not count
 //
+// lse is a maximum plus a logarithm, and one fp32 number loses of the logarithm what is below the maximum's last place: all of it where a row
+// holds nothing but the type's lowest value.  So logp is formed of the two apart, (x_label - max) - log(sum), lse can be left with its low part
+// (lse + low = max + log(sum) to twice the bits), and where a backward call is given no low part, rows whose lse has a last place that matters
+// form maximum and sum anew.
+//
 // A row is read once forward (running maximum and sum) and once backward; rows that do not count are not read at all.  Vocabularies may
 // be odd, so a row may begin anywhere: the elements up to the first 16-byte boundary and behind the last one are taken one by one.
 // Bound by bytes; the exponentials take about a third of the vector units' time beside them.  In bf16, a third of the tokens not counted:
@@ -76,16 +81,38 @@ __device__ __forceinline__ Running join(Running r, float2* s_part)
     return {all, row16_sum(v.y * exp_of(v.x - reference(all)))};
 }
 
-__device__ __forceinline__ void finish(const Running& r, float x_label, int64_t t, float* logp, float* lse)
+// lse, and with LOW its low part.  (Kernels of their own, as an argument more costs the calls without it up to 0.6 us: it is read from another line of
+// the arguments' memory.)
+template <bool LOW, typename F> struct Lse {
+    F* hi;
+    __device__ __forceinline__ void put(int64_t t, float l, float) const { hi[t] = l; }
+    __device__ __forceinline__ float low(int64_t) const { return 0.0f; }
+};
+template <typename F> struct Lse<true, F> {
+    F *hi, *lo;
+    __device__ __forceinline__ void put(int64_t t, float l, float low) const { hi[t] = l; lo[t] = low; }
+    __device__ __forceinline__ float low(int64_t t) const { return lo[t]; }
+};
+template <bool LOW, typename F>
+Lse<LOW, F> lse_of(F* hi, F* lo)
 {
-    const float l = reference(r.m) + logf(r.s);
-    lse[t] = l;
-    logp[t] = x_label == -INFINITY && l == l ? -INFINITY : x_label - l;
+    if constexpr (LOW) return {hi, lo};
+    else return {hi};
 }
 
-template <typename T>
+template <bool LOW>
+__device__ __forceinline__ void finish(const Running& r, float x_label, int64_t t, float* logp, Lse<LOW, float> lse)
+{
+    const float m = reference(r.m), log_s = logf(r.s), l = m + log_s;
+    const float added = l - m;                                        // what rounding took from m + log_s, exactly
+    const float low = (m - (l - added)) + (log_s - added);
+    lse.put(t, l, fabsf(l) < INFINITY ? low : 0.0f);
+    logp[t] = x_label == -INFINITY && l == l ? -INFINITY : (x_label - m) - log_s;
+}
+
+template <typename T, bool LOW>
 __global__ void __launch_bounds__(1024)
-token_logprob_kernel(const T* __restrict__ logits, int64_t ld, int V, const int64_t* __restrict__ labels, float* __restrict__ logp, float* __restrict__ lse,
+token_logprob_kernel(const T* __restrict__ logits, int64_t ld, int V, const int64_t* __restrict__ labels, float* __restrict__ logp, Lse<LOW, float> lse,
                      float2* __restrict__ partial)
 {
     constexpr int E = kPiece<T>;
@@ -94,7 +121,10 @@ token_logprob_kernel(const T* __restrict__ logits, int64_t ld, int V, const int6
     const int64_t label = labels[t];
     const int split = blockIdx.y, splits = gridDim.y;
     if (label < 0 || label >= V) {
-        if (split == 0 && threadIdx.x == 0) logp[t] = lse[t] = 0.0f;
+        if (split == 0 && threadIdx.x == 0) {
+            logp[t] = 0.0f;
+            lse.put(t, 0.0f, 0.0f);
+        }
         return;
     }
     const Row<T> row(logits + t * ld, V);
@@ -132,10 +162,10 @@ token_logprob_kernel(const T* __restrict__ logits, int64_t ld, int V, const int6
 }
 
 // one wave a row: the parts of its splits
-template <typename T>
+template <typename T, bool LOW>
 __global__ void __launch_bounds__(256)
 token_join_kernel(const T* __restrict__ logits, int64_t ld, int64_t rows, int V, const int64_t* __restrict__ labels, const float2* __restrict__ partial, int splits,
-                  float* __restrict__ logp, float* __restrict__ lse)
+                  float* __restrict__ logp, Lse<LOW, float> lse)
 {
     const int64_t t = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -148,32 +178,63 @@ token_join_kernel(const T* __restrict__ logits, int64_t ld, int64_t rows, int V,
     if (lane == 0) finish(Running{m, s}, element(logits + t * ld + label), t, logp, lse);
 }
 
-template <typename T, bool PAST>
+// Sizes of lse from which half of its last place, 2^-18 of a probability and more, is more than the rest of the arithmetic loses.
+constexpr float kCoarse = 64.0f;
+constexpr int kChunk = 1024;                                          // pieces of a row that a workgroup writes
+
+template <typename T, bool PAST, bool LOW>
 __global__ void __launch_bounds__(256)
-token_logprob_bwd_kernel(const float* __restrict__ d_logp, const T* logits, int64_t ld, int V, const int64_t* __restrict__ labels, const float* __restrict__ lse,
-                         T* out, int64_t ld_out, int chunk)
+token_logprob_bwd_kernel(const float* __restrict__ d_logp, const T* logits, int64_t ld, int V, const int64_t* __restrict__ labels, Lse<LOW, const float> lse,
+                         T* out, int64_t ld_out)
 {
     constexpr int E = kPiece<T>;
+    __shared__ float2 s_part[16];
     const int64_t t = blockIdx.x;
     const int64_t label = labels[t];
     const bool counts = label >= 0 && label < V;
-    const float l = counts ? lse[t] : 0.0f, d = counts ? d_logp[t] : 0.0f;
+    float l = counts ? lse.hi[t] : 0.0f, low = counts ? lse.low(t) : 0.0f;
+    const float d = counts ? d_logp[t] : 0.0f;
     const bool nothing = !counts || l == -INFINITY;                   // no gradient: written without a look at the logits
     const Row<T> row(logits + t * ld, V), dst(out + t * ld_out, V);
+    const int tid = static_cast<int>(threadIdx.x);
+    int from = static_cast<int>(blockIdx.y) * kChunk, to_piece = min(dst.pieces, from + kChunk);
+    if (!LOW && __builtin_expect(!nothing && fabsf(l) >= kCoarse && fabsf(l) < INFINITY, 0)) {
+        // The workgroup takes the whole row, as its results may lie over what the sum reads.
+        if (blockIdx.y != 0) return;
+        to_piece = dst.pieces;
+        Running r{-INFINITY, 0.0f};
+        for (int i = tid; i < row.pieces; i += 256) {
+            float f[E];
+            load_piece(row.p + row.head + static_cast<int64_t>(i) * E, f);
+            take(r, f);
+        }
+        if (tid < row.head) {
+            const float f[1] = {element(row.p + tid)};
+            take(r, f);
+        }
+        if (tid < V - row.tail()) {
+            const float f[1] = {element(row.p + row.tail() + tid)};
+            take(r, f);
+        }
+        r = join(r, s_part);                                          // its barrier stands between the reads and the writes below
+        l = reference(r.m);
+        low = logf(r.s);
+    }
+    const float low2 = low * kLog2e;
+    auto probability = [&](float x) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x - l, kLog2e, -low2)); };
     // pieces of the row that is written; what is read may lie otherwise
     const bool alike = dst.head == row.head;
     T* const to = out + t * ld_out;
     auto value = [&](int v) {
         if (nothing) return 0.0f;
-        const float p = exp_of(element(row.p + v) - l);
+        const float p = probability(element(row.p + v));
         return v == static_cast<int>(label) ? d * (1.0f - p) : -d * p;
     };
     if (blockIdx.y == 0) {
-        if (static_cast<int>(threadIdx.x) < dst.head) put(to + threadIdx.x, value(threadIdx.x));
-        if (static_cast<int>(threadIdx.x) < V - dst.tail()) put(to + dst.tail() + threadIdx.x, value(dst.tail() + threadIdx.x));
+        if (tid < dst.head) put(to + tid, value(tid));
+        if (tid < V - dst.tail()) put(to + dst.tail() + tid, value(dst.tail() + tid));
     }
-    const int end = min(dst.pieces, (static_cast<int>(blockIdx.y) + 1) * chunk);
-    for (int i = static_cast<int>(blockIdx.y) * chunk + static_cast<int>(threadIdx.x); i < end; i += 256) {
+    for (int i = from + tid; i < to_piece; i += 256) {
         const int v = dst.head + i * E;
         float f[E] = {};
         if (!nothing) {
@@ -186,7 +247,7 @@ token_logprob_bwd_kernel(const float* __restrict__ d_logp, const T* logits, int6
             const int at = static_cast<int>(label) - v;
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                const float p = exp_of(f[k] - l);
+                const float p = probability(f[k]);
                 f[k] = k == at ? d * (1.0f - p) : -d * p;
             }
         }
@@ -337,25 +398,27 @@ preference_mean_kernel(const float* __restrict__ pair_loss, int P, float* __rest
     if (threadIdx.x == 0) *loss = static_cast<float>(sum / P);
 }
 
-template <typename T>
+template <typename T, bool LOW>
 void fwd(const TokenLogprob& a, int splits, hipStream_t stream)
 {
     const T* const logits = static_cast<const T*>(a.logits);
     const int V = static_cast<int>(a.V);
     const dim3 grid(static_cast<unsigned>(a.T), static_cast<unsigned>(splits));
-    token_logprob_kernel<T><<<grid, a.T < 1024 && a.V >= 8192 ? 1024 : 256, 0, stream>>>(logits, a.ld, V, a.labels, a.logp, a.lse, a.partial);
+    const auto lse = lse_of<LOW>(a.lse, a.lse_low);
+    token_logprob_kernel<T, LOW><<<grid, a.T < 1024 && a.V >= 8192 ? 1024 : 256, 0, stream>>>(logits, a.ld, V, a.labels, a.logp, lse, a.partial);
     if (splits > 1)
-        token_join_kernel<T><<<static_cast<unsigned>((a.T + 3) / 4), 256, 0, stream>>>(logits, a.ld, a.T, V, a.labels, a.partial, splits, a.logp, a.lse);
+        token_join_kernel<T, LOW><<<static_cast<unsigned>((a.T + 3) / 4), 256, 0, stream>>>(logits, a.ld, a.T, V, a.labels, a.partial, splits, a.logp, lse);
 }
 
-template <typename T>
+template <typename T, bool LOW>
 void bwd(const TokenLogprobBwd& a, hipStream_t stream)
 {
-    const int pieces = static_cast<int>((a.V + kPiece<T> - 1) / kPiece<T>), chunk = 1024;
-    const dim3 grid(static_cast<unsigned>(a.T), static_cast<unsigned>((pieces + chunk - 1) / chunk));
+    const int pieces = static_cast<int>((a.V + kPiece<T> - 1) / kPiece<T>);
+    const dim3 grid(static_cast<unsigned>(a.T), static_cast<unsigned>((pieces + kChunk - 1) / kChunk));
     const bool past = a.T * a.V * static_cast<int64_t>(sizeof(T)) > kPastCaches;       // 8192 x 32000 in bf16: 178 to 172 us
-    const auto kernel = past ? &token_logprob_bwd_kernel<T, true> : &token_logprob_bwd_kernel<T, false>;
-    kernel<<<grid, 256, 0, stream>>>(a.d_logp, static_cast<const T*>(a.logits), a.ld, static_cast<int>(a.V), a.labels, a.lse, static_cast<T*>(a.out), a.ld_out, chunk);
+    const auto kernel = past ? &token_logprob_bwd_kernel<T, true, LOW> : &token_logprob_bwd_kernel<T, false, LOW>;
+    kernel<<<grid, 256, 0, stream>>>(a.d_logp, static_cast<const T*>(a.logits), a.ld, static_cast<int>(a.V), a.labels, lse_of<LOW>(a.lse, a.lse_low),
+                                     static_cast<T*>(a.out), a.ld_out);
 }
 
 }  // namespace
@@ -371,13 +434,15 @@ int token_splits(int64_t T, int64_t V)
 hipError_t launch_token_logprob(const TokenLogprob& a, bool f32, hipStream_t stream)
 {
     const int splits = token_splits(a.T, a.V);
-    f32 ? fwd<float>(a, splits, stream) : fwd<uint16_t>(a, splits, stream);
+    if (a.lse_low) f32 ? fwd<float, true>(a, splits, stream) : fwd<uint16_t, true>(a, splits, stream);
+    else f32 ? fwd<float, false>(a, splits, stream) : fwd<uint16_t, false>(a, splits, stream);
     return hipGetLastError();
 }
 
 hipError_t launch_token_logprob_bwd(const TokenLogprobBwd& a, bool f32, hipStream_t stream)
 {
-    f32 ? bwd<float>(a, stream) : bwd<uint16_t>(a, stream);
+    if (a.lse_low) f32 ? bwd<float, true>(a, stream) : bwd<uint16_t, true>(a, stream);
+    else f32 ? bwd<float, false>(a, stream) : bwd<uint16_t, false>(a, stream);
     return hipGetLastError();
 }
 

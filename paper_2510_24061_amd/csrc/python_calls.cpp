@@ -374,39 +374,40 @@ PyObject* mx4_linear(PyObject*, PyObject* const* args, Py_ssize_t count)
 PyObject* token_logprob(PyObject*, PyObject* const* args, Py_ssize_t count)
 {
     return guarded([&]() -> PyObject* {
-        Args a(args, count, 6);
-        const at::Tensor *x = a.rows(), *labels = a.tensor(), *logp = a.tensor(), *lse = a.tensor(), *ws = a.tensor();
+        Args a(args, count, 7);
+        const at::Tensor *x = a.rows(), *labels = a.tensor(), *logp = a.tensor(), *lse = a.tensor(), *ws = a.tensor(), *low = a.tensor();
         void* const stream = a.address();
         a.need(x, "logits");
         if (a.failed()) return nullptr;
         const int64_t T = x->size(0), V = x->size(1), ld = stride(x);
         const falqon_dtype lt = a.dtype(x, FALQON_BF16);
-        a.expect(labels, at::kLong, {T}, "labels"); a.expect(logp, at::kFloat, {T}, "logp"); a.expect(lse, at::kFloat, {T}, "lse");
+        a.expect(labels, at::kLong, {T}, "labels"); a.expect(logp, at::kFloat, {T}, "logp"); a.expect(lse, at::kFloat, {T}, "lse"); a.expect(low, at::kFloat, {T}, "lse_low");
         if (a.failed()) return nullptr;
         void *const px = data(x), *const pw = data(ws);
         const int64_t* const pl = data<int64_t>(labels);
-        float *const pp = data<float>(logp), *const ps = data<float>(lse);
+        float *const pp = data<float>(logp), *const ps = data<float>(lse), *const plow = data<float>(low);
         const size_t size = bytes(ws);
-        return status_of([=] { return falqon_token_logprob(px, lt, T, V, ld, pl, pp, ps, pw, size, stream); });
+        return status_of([=] { return falqon_token_logprob_low(px, lt, T, V, ld, pl, pp, ps, plow, pw, size, stream); });
     });
 }
 
 PyObject* token_logprob_bwd(PyObject*, PyObject* const* args, Py_ssize_t count)
 {
     return guarded([&]() -> PyObject* {
-        Args a(args, count, 6);
-        const at::Tensor *d = a.tensor(), *x = a.rows(), *labels = a.tensor(), *lse = a.tensor(), *out = a.rows();
+        Args a(args, count, 7);
+        const at::Tensor *d = a.tensor(), *x = a.rows(), *labels = a.tensor(), *lse = a.tensor(), *out = a.rows(), *low = a.tensor();
         void* const stream = a.address();
         a.need(x, "logits");
         if (a.failed()) return nullptr;
         const int64_t T = x->size(0), V = x->size(1), ld = stride(x), ld_d = stride(out);
         const falqon_dtype lt = a.dtype(x, FALQON_BF16);
         a.expect(d, at::kFloat, {T}, "d_logp"); a.expect(labels, at::kLong, {T}, "labels"); a.expect(lse, at::kFloat, {T}, "lse"); a.expect(out, x->scalar_type(), {T, V}, "dlogits");
+        a.expect(low, at::kFloat, {T}, "lse_low");
         if (a.failed()) return nullptr;
         void *const px = data(x), *const po = data(out);
         const int64_t* const pl = data<int64_t>(labels);
-        float *const pd = data<float>(d), *const ps = data<float>(lse);
-        return status_of([=] { return falqon_token_logprob_bwd(pd, px, lt, T, V, ld, pl, ps, po, ld_d, stream); });
+        float *const pd = data<float>(d), *const ps = data<float>(lse), *const plow = data<float>(low);
+        return status_of([=] { return falqon_token_logprob_bwd_low(pd, px, lt, T, V, ld, pl, ps, plow, po, ld_d, stream); });
     });
 }
 
