@@ -523,7 +523,8 @@ falqon_status falqon_token_logprob_bwd_low(const float* d_logp, const void* logi
  *   d_logp_t  = d loss / d logp_t, the same for all tokens of a sequence; 0 for tokens of none
  *
  *   offsets   in   int64 [2 P + 1], ascending (bounds outside [0, T] are taken as the nearest inside); empty sequences are allowed
- *   logp, ref_logp  in  fp32 [T], 0 for tokens that do not count
+ *   logp, ref_logp  in  fp32 [T], 0 for tokens that do not count.  A logp of -infinity (a masked label) makes its reward -infinity and the pair's loss
+ *             infinite, or without smoothing 0 where it is the rejected one's; a reward without a value (both -infinity) makes the loss NaN
  *   loss, rewards, d_logp  out  fp32 [1], [2, P], [T]
  * 0 <= smoothing < 0.5, beta finite; 1 <= P <= 65536.  ws: falqon_logprob_workspace_bytes(T, 1, P) bytes.
  */

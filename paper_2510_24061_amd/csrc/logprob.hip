@@ -310,7 +310,8 @@ struct Preference {
         return o < 0 ? 0 : o > T ? T : o;
     }
     // of one pair's loss, and of the loss by its chosen reward's sum of log-probabilities
-    __device__ __forceinline__ float term(float z) const { return (1.0f - smoothing) * softplus(-z) + smoothing * softplus(z); }
+    // (z is infinite where a label was masked: without smoothing the second part is then 0, not 0 times infinity)
+    __device__ __forceinline__ float term(float z) const { return (1.0f - smoothing) * softplus(-z) + (smoothing > 0.0f ? smoothing * softplus(z) : 0.0f); }
     __device__ __forceinline__ float slope(float z) const { return beta / static_cast<float>(P) * (smoothing * logistic(z) - (1.0f - smoothing) * logistic(-z)); }
 };
 
