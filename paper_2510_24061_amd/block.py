@@ -4,6 +4,8 @@ stream, SwiGLU from 8-bit checkpoints, frozen linear layers on 4-bit codes, log-
 Plumbing only: every computation is a C-ABI call.  The melded layers keep nothing of their inputs but O_A, so with the
 checkpoints here a block's saved activations are those of its attention, one byte and 1/32 for each element of the norms' streams,
 of gate and of up.
+
+First derivatives only: under create_graph gradients come as ever, and following them (a penalty on a gradient) raises RuntimeError.
 """
 from typing import Optional, Sequence, Tuple
 
@@ -29,6 +31,36 @@ def _codes(T: int, n: int, dev) -> Tuple[torch.Tensor, torch.Tensor]:
     return torch.empty(T, n, dtype=_U8, device=dev), torch.empty(T, (n + 31) // 32, dtype=_U8, device=dev)
 
 
+class _Refused(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tie, *grads):
+        return grads
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the kernels around the melded layers have first derivatives only: their gradients cannot be differentiated")
+
+
+def _tie(x: torch.Tensor) -> torch.Tensor:
+    """The last output of a function here, saved last: it holds nothing, and stands for the function in the graph of its gradients."""
+    return torch.empty(0, dtype=torch.float32, device=x.device)
+
+
+def _first_order(backward):
+    """A backward pass of kernels.  Under create_graph its gradients depend on the function's inputs through a node that refuses to be followed;
+    with no graph a penalty on them would be dropped without a word."""
+
+    def run(ctx, *grads):
+        with torch.no_grad():
+            out = backward(ctx, *grads[:-1])
+        if not torch.is_grad_enabled():
+            return out
+        again = iter(_Refused.apply(ctx.saved_tensors[-1], *(v.detach() for v in out if isinstance(v, torch.Tensor))))
+        return tuple(next(again) if isinstance(v, torch.Tensor) else v for v in out)
+
+    return run
+
+
 class _NormFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, b, w, w_post, gate, scale, eps, checkpoint):
@@ -47,15 +79,16 @@ class _NormFn(torch.autograd.Function):
         _b.norm_fwd(x2, w, h, rstd, b=b2, s=s, scale=scale, gate=gate, w_post=w_post, rstd_b=rstd_b, sq=sq, s_exp=s_exp, bq=bq, b_exp=b_exp, eps=eps)
         saved_s = sq if checkpoint else x2 if s is None else s
         saved_b = None if not reads_b else bq if checkpoint else b2
-        ctx.save_for_backward(saved_s, s_exp, saved_b, b_exp, rstd, rstd_b, w, w_post, gate)
+        ctx.save_for_backward(saved_s, s_exp, saved_b, b_exp, rstd, rstd_b, w, w_post, gate, tie := _tie(x))
         ctx.scale, ctx.shape, ctx.branch = scale, x.shape, b is not None
         h = h.reshape(x.shape)
-        return h if s is None else (s.reshape(x.shape), h)
+        return (h, tie) if s is None else (s.reshape(x.shape), h, tie)
 
     @staticmethod
+    @_first_order
     def backward(ctx, *grads):
         ds, dh = (None, grads[0]) if not ctx.branch else grads
-        s, s_exp, b, b_exp, rstd, rstd_b, w, w_post, gate = ctx.saved_tensors
+        s, s_exp, b, b_exp, rstd, rstd_b, w, w_post, gate, _ = ctx.saved_tensors
         T, d, dev = s.shape[0], s.shape[1], s.device
         dh2 = torch.zeros(T, d, dtype=w.dtype, device=dev) if dh is None else _rows(dh)
         ds2 = None if ds is None else _rows(ds)
@@ -88,8 +121,8 @@ class BlockNorm(torch.nn.Module):
 
     def forward(self, x: torch.Tensor, branch: Optional[torch.Tensor] = None):
         if branch is None:
-            return x, _NormFn.apply(x, None, self.weight, None, None, 1.0, self.eps, self.checkpoint)
-        return _NormFn.apply(x, branch, self.weight, self.post_weight, self.gate, self.scale, self.eps, self.checkpoint)
+            return x, _NormFn.apply(x, None, self.weight, None, None, 1.0, self.eps, self.checkpoint)[0]
+        return _NormFn.apply(x, branch, self.weight, self.post_weight, self.gate, self.scale, self.eps, self.checkpoint)[:2]
 
 
 class _SwigluFn(torch.autograd.Function):
@@ -102,12 +135,13 @@ class _SwigluFn(torch.autograd.Function):
         if checkpoint:
             (gq, g_exp), (uq, u_exp) = _codes(T, m, g.device), _codes(T, m, g.device)
         _b.swiglu_fwd(g2, u2, h, gq=gq, g_exp=g_exp, uq=uq, u_exp=u_exp)
-        ctx.save_for_backward(gq if checkpoint else g2, uq if checkpoint else u2, g_exp, u_exp)
-        return h.reshape(g.shape)
+        ctx.save_for_backward(gq if checkpoint else g2, uq if checkpoint else u2, g_exp, u_exp, tie := _tie(g))
+        return h.reshape(g.shape), tie
 
     @staticmethod
+    @_first_order
     def backward(ctx, dh):
-        g, u, g_exp, u_exp = ctx.saved_tensors
+        g, u, g_exp, u_exp, _ = ctx.saved_tensors
         dh2 = _rows(dh)
         dg, du = (torch.empty(dh2.shape, dtype=dh.dtype, device=dh.device) for _ in range(2))
         _b.swiglu_bwd(dh2, g, u, dg, du, g_exp=g_exp, u_exp=u_exp)
@@ -116,7 +150,7 @@ class _SwigluFn(torch.autograd.Function):
 
 def swiglu(g: torch.Tensor, u: torch.Tensor, checkpoint: bool = True) -> torch.Tensor:
     """silu(g) * u; with `checkpoint`, g and u are kept for the backward pass in 8 bits."""
-    return _SwigluFn.apply(g, u, checkpoint)
+    return _SwigluFn.apply(g, u, checkpoint)[0]
 
 
 class _TokenLogprobFn(torch.autograd.Function):
@@ -128,13 +162,14 @@ class _TokenLogprobFn(torch.autograd.Function):
         logp, lse, low = (torch.empty(T, dtype=torch.float32, device=x.device) for _ in range(3))
         l2 = labels.reshape(-1).contiguous()
         _b.token_logprob(x, l2, logp, lse, torch.empty(_b.logprob_workspace_bytes(T, V), dtype=_U8, device=x.device), lse_low=low)
-        ctx.save_for_backward(x, l2, lse, low)
+        ctx.save_for_backward(x, l2, lse, low, tie := _tie(x))
         ctx.shape = logits.shape
-        return logp.reshape(labels.shape)
+        return logp.reshape(labels.shape), tie
 
     @staticmethod
+    @_first_order
     def backward(ctx, d_logp):
-        x, labels, lse, low = ctx.saved_tensors
+        x, labels, lse, low, _ = ctx.saved_tensors
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         _b.token_logprob_bwd(d_logp.reshape(-1).contiguous(), x, labels, lse, dx, lse_low=low)
         return dx.reshape(ctx.shape), None
@@ -142,7 +177,7 @@ class _TokenLogprobFn(torch.autograd.Function):
 
 def token_logprobs(logits: torch.Tensor, labels: torch.Tensor) -> torch.Tensor:
     """log softmax(logits)[label] for logits [..., V] and int64 labels [...], fp32; labels outside the vocabulary (-100) give 0."""
-    return _TokenLogprobFn.apply(logits, labels)
+    return _TokenLogprobFn.apply(logits, labels)[0]
 
 
 class _PreferenceFn(torch.autograd.Function):
@@ -152,20 +187,21 @@ class _PreferenceFn(torch.autograd.Function):
         T, P, dev = p2.shape[0], (offsets.shape[0] - 1) // 2, logp.device
         loss, rewards, d = torch.empty(1, device=dev), torch.empty(2, P, device=dev), torch.empty(T, device=dev)
         _b.preference_loss(p2, r2, offsets, loss, rewards, d, torch.empty(_b.logprob_workspace_bytes(T, 1, P), dtype=_U8, device=dev), beta=beta, smoothing=smoothing)
-        ctx.save_for_backward(d)
+        ctx.save_for_backward(d, tie := _tie(d))
         ctx.shape = logp.shape
         ctx.mark_non_differentiable(rewards)
-        return loss[0], rewards
+        return loss[0], rewards, tie
 
     @staticmethod
-    def backward(ctx, d_loss, _):
-        d, = ctx.saved_tensors
+    @_first_order
+    def backward(ctx, d_loss, d_rewards):
+        d, _ = ctx.saved_tensors
         return (d * d_loss).reshape(ctx.shape), None, None, None, None
 
 
 def preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor, offsets: torch.Tensor, beta: float = 0.1, smoothing: float = 0.0):
     """Loss and rewards [2, P] of the sequences that `offsets` (int64 [2 P + 1], on the GPU) cuts the tokens into: chosen, then rejected."""
-    return _PreferenceFn.apply(logp, ref_logp, offsets, beta, smoothing)
+    return _PreferenceFn.apply(logp, ref_logp, offsets, beta, smoothing)[:2]
 
 
 def _mx4(t: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -198,9 +234,11 @@ class _Mx4Fn(torch.autograd.Function):
             outs.append(y.reshape(*x.shape[:-1], l.out_features))
         ctx.layers, ctx.shape, ctx.dtype = layers, x.shape, x.dtype
         ctx.set_materialize_grads(False)
-        return tuple(outs)
+        ctx.save_for_backward(tie := _tie(x))
+        return (*outs, tie)
 
     @staticmethod
+    @_first_order
     def backward(ctx, *dys):
         if not ctx.needs_input_grad[0]:
             return (None,) * (1 + len(ctx.layers))
@@ -254,7 +292,7 @@ class Mx4Group:
         self.layers = list(layers)
 
     def __call__(self, x: torch.Tensor):
-        return _Mx4Fn.apply(x, *self.layers)
+        return _Mx4Fn.apply(x, *self.layers)[:-1]
 
 
 def _group(layers: Sequence[torch.nn.Module]):

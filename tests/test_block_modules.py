@@ -1,0 +1,150 @@
+"""Modules and functions around the melded layers on the CPU: what they hand to the library's calls, which are replaced here by plain torch forms."""
+import pytest
+import torch
+
+from paper_2510_24061_amd import block
+
+
+class Calls:
+    """Plain forms of the calls, with the binding's checks of shapes, and a record of what was asked for."""
+
+    MX_E2M1 = 1
+
+    def __init__(self):
+        self.asked = []
+
+    def norm_workspace_bytes(self, T, d):
+        return 16
+
+    def logprob_workspace_bytes(self, T, V, P=1):
+        return 16
+
+    def norm_fwd(self, x, w, h, rstd, b=None, s=None, scale=1.0, gate=None, w_post=None, rstd_b=None, sq=None, s_exp=None, bq=None, b_exp=None, eps=1e-5):
+        self.asked.append(("norm_fwd", sq is not None, bq is not None))
+        v = x.float()
+        if b is not None:
+            assert b.shape == x.shape
+            u = b.float()
+            if w_post is not None:
+                rstd_b.copy_((u.square().mean(1) + eps).rsqrt())
+                u = u * rstd_b[:, None] * w_post.float()
+            v = v + scale * u * (1.0 if gate is None else gate.float())
+            s.copy_(v)
+        rstd.copy_((v.square().mean(1) + eps).rsqrt())
+        h.copy_(v * rstd[:, None] * w.float())
+
+    def norm_bwd(self, dh, s, w, rstd, dx, ds=None, b=None, db=None, scale=1.0, gate=None, w_post=None, rstd_b=None, s_exp=None, b_exp=None, dw=None, dw_post=None,
+                 dgate=None, ws=None):
+        self.asked.append(("norm_bwd", dh, ds))
+        hat = s.float() * rstd[:, None]
+        g = w.float() * dh.float()
+        dx.copy_(rstd[:, None] * (g - hat * (g * hat).mean(1, keepdim=True)) + (0.0 if ds is None else ds.float()))
+        if db is not None:
+            db.copy_(scale * dx.float())
+        if dw is not None:
+            dw.copy_((dh.float() * hat).sum(0))
+
+    def swiglu_fwd(self, g, u, h, gq=None, g_exp=None, uq=None, u_exp=None):
+        assert g.shape == u.shape == h.shape
+        self.asked.append(("swiglu_fwd", gq is not None, g.data_ptr() % 16 == 0 and u.data_ptr() % 16 == 0))
+        h.copy_(torch.nn.functional.silu(g.float()) * u.float())
+
+    def swiglu_bwd(self, dh, g, u, dg, du, g_exp=None, u_exp=None):
+        s = torch.sigmoid(g.float())
+        dg.copy_(dh.float() * u.float() * s * (1 + g.float() * (1 - s)))
+        du.copy_(dh.float() * g.float() * s)
+
+    def token_logprob(self, logits, labels, logp, lse, ws, lse_low=None):
+        assert logits.stride(0) >= logits.shape[1] or logits.shape[0] == 1
+        assert labels.shape == logp.shape == (logits.shape[0],)
+        counts = (labels >= 0) & (labels < logits.shape[1])
+        lse.copy_(torch.logsumexp(logits.float(), 1) * counts)
+        logp.copy_((logits.float().gather(1, labels.clamp(0, logits.shape[1] - 1)[:, None])[:, 0] - lse) * counts)
+        if lse_low is not None:
+            lse_low.zero_()
+
+    def token_logprob_bwd(self, d_logp, logits, labels, lse, dlogits, lse_low=None):
+        p = torch.softmax(logits.float(), 1).neg()
+        p[torch.arange(len(labels)), labels] += 1.0
+        dlogits.copy_(d_logp[:, None] * p)
+
+    def preference_loss(self, logp, ref_logp, offsets, loss, rewards, d_logp, ws, beta=0.1, smoothing=0.0):
+        assert all(t.dtype == torch.float32 for t in (logp, ref_logp, loss, rewards, d_logp))
+        o, P = offsets.tolist(), rewards.shape[1]
+        with torch.enable_grad():
+            p = logp.detach().requires_grad_()
+            r = beta * torch.stack([(p[a:b] - ref_logp[a:b]).sum() for a, b in zip(o, o[1:])]).reshape(2, P)
+            value = torch.nn.functional.softplus(r[1] - r[0]).mean()
+            d_logp.copy_(torch.autograd.grad(value, p)[0])
+        loss.fill_(value.item())
+        rewards.copy_(r.detach())
+
+
+for _name in ("norm_fwd", "norm_bwd", "swiglu_fwd", "swiglu_bwd", "token_logprob", "token_logprob_bwd", "preference_loss"):
+    setattr(Calls, _name, torch.no_grad()(getattr(Calls, _name)))               # autograd does not see a kernel's work
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    c = Calls()
+    monkeypatch.setattr(block, "_b", c)
+    return c
+
+
+def norm(d, **kw):
+    return block.BlockNorm(d, dtype=torch.float32, device="cpu", **kw)
+
+
+# ---- derivatives of the derivatives ---------------------------------------------------------------------------------------------
+def first_order(name):
+    """(differentiable inputs, output) of one of the functions"""
+    g = torch.Generator().manual_seed(1)
+    t = lambda *s: torch.randn(*s, generator=g, requires_grad=True)  # noqa: E731
+    if name == "norm":
+        x, b = t(3, 32), t(3, 32)
+        return (x, b), norm(32, checkpoint=False)(x, b)[1].sum()
+    if name == "swiglu":
+        x, y = t(3, 32), t(3, 32)
+        return (x, y), block.swiglu(x, y, checkpoint=False).sum()
+    if name == "logprobs":
+        x = t(3, 7)
+        return (x,), block.token_logprobs(x, torch.tensor([1, 2, 3])).sum()
+    if name == "loss":
+        x = t(6)
+        return (x,), block.preference_loss(x, torch.zeros(6), torch.tensor([0, 3, 6]))[0]
+    x = t(3, 32)
+    layer = block.Mx4Linear.__new__(block.Mx4Linear)
+    torch.nn.Module.__init__(layer)
+    layer.in_features, layer.out_features = 32, 16
+    layer.wq, layer.w_exp, layer.wtq, layer.wt_exp = (torch.zeros(1) for _ in range(4))
+    return (x,), layer(x).float().square().sum()
+
+
+@pytest.mark.parametrize("name", ["norm", "swiglu", "logprobs", "loss", "mx4"])
+@pytest.mark.parametrize("through_loss", [False, True])
+def test_a_second_derivative_is_refused(calls, monkeypatch, name, through_loss):
+    """Under create_graph the first derivatives come as before; a penalty on them is refused, not dropped (plain forms beside it count as ever)."""
+    monkeypatch.setattr(block, "_mx4_product", lambda x2, wq, w_exp, m, codes=None: (torch.ones(3, m, dtype=torch.bfloat16), (x2, None)))
+    inputs, out = first_order(name)
+    plain = torch.autograd.grad(out, inputs, retain_graph=True)
+    value = out.square() if through_loss else out
+    grads = torch.autograd.grad(value, inputs, create_graph=True)
+    factor = 2 * out.detach() if through_loss and name != "mx4" else 1.0       # the product's stand-in gives ones
+    assert all(torch.allclose(a, b * factor) and a.requires_grad for a, b in zip(grads, plain))
+    own = inputs[0].square().sum()
+    with pytest.raises(RuntimeError, match="differentiat"):
+        torch.autograd.grad(own + sum(v.square().sum() for v in grads), inputs)
+
+
+def test_create_graph_without_a_second_derivative(calls):
+    x, y = torch.randn(2, 32, requires_grad=True), torch.randn(2, 32, requires_grad=True)
+    block.swiglu(x, y, checkpoint=False).sum().backward(create_graph=True)
+    want = torch.autograd.grad((torch.nn.functional.silu(x) * y).sum(), (x, y))
+    assert torch.allclose(x.grad, want[0], atol=1e-6) and torch.allclose(y.grad, want[1], atol=1e-6)
+
+
+def test_only_what_is_asked_for(calls):
+    """An input without a gradient gets none, also where the other has one."""
+    x, y = torch.randn(2, 32, requires_grad=True), torch.randn(2, 32)
+    g, = torch.autograd.grad(block.swiglu(x, y, checkpoint=False).sum(), x, create_graph=True)
+    assert g.shape == x.shape and y.grad is None
