@@ -185,7 +185,7 @@ class _PreferenceFn(torch.autograd.Function):
     def forward(ctx, logp, ref_logp, offsets, beta, smoothing):
         p2, r2 = logp.reshape(-1).contiguous(), ref_logp.reshape(-1).contiguous()
         T, P, dev = p2.shape[0], (offsets.shape[0] - 1) // 2, logp.device
-        loss, rewards, d = torch.empty(1, device=dev), torch.empty(2, P, device=dev), torch.empty(T, device=dev)
+        loss, rewards, d = (torch.empty(s, dtype=torch.float32, device=dev) for s in (1, (2, P), T))
         _b.preference_loss(p2, r2, offsets, loss, rewards, d, torch.empty(_b.logprob_workspace_bytes(T, 1, P), dtype=_U8, device=dev), beta=beta, smoothing=smoothing)
         ctx.save_for_backward(d, tie := _tie(d))
         ctx.shape = logp.shape

@@ -148,3 +148,14 @@ def test_only_what_is_asked_for(calls):
     x, y = torch.randn(2, 32, requires_grad=True), torch.randn(2, 32)
     g, = torch.autograd.grad(block.swiglu(x, y, checkpoint=False).sum(), x, create_graph=True)
     assert g.shape == x.shape and y.grad is None
+
+
+def test_loss_under_another_default_type(calls):
+    """The loss's buffers are fp32 whatever torch's default is."""
+    kept = torch.get_default_dtype()
+    torch.set_default_dtype(torch.bfloat16)
+    try:
+        loss, rewards = block.preference_loss(torch.zeros(6, dtype=torch.float32), torch.zeros(6, dtype=torch.float32), torch.tensor([0, 3, 6]))
+    finally:
+        torch.set_default_dtype(kept)
+    assert loss.dtype == rewards.dtype == torch.float32
