@@ -67,6 +67,7 @@ class _NormFn(torch.autograd.Function):
         ctx.set_materialize_grads(False)
         x2, b2 = _rows(x), None if b is None else _rows(b)
         T, d, dev, dt = x2.shape[0], x2.shape[1], x.device, x.dtype
+        checkpoint = checkpoint and any(ctx.needs_input_grad)
         h, rstd = torch.empty(T, d, dtype=dt, device=dev), torch.empty(T, dtype=torch.float32, device=dev)
         s = None if b is None else torch.empty(T, d, dtype=dt, device=dev)
         rstd_b = None if w_post is None else torch.empty(T, dtype=torch.float32, device=dev)
@@ -108,7 +109,7 @@ class BlockNorm(torch.nn.Module):
     """Joins a branch to the residual stream and normalizes the stream:  stream, h = norm(x, branch).
 
     s = x + scale * gate * u with u the branch, or with `post_norm` RMSNorm(branch); h = RMSNorm(s).  Without a branch s is x.
-    `checkpoint` keeps the backward pass's inputs in 8 bits.  Weights are trained if `trainable`."""
+    `checkpoint` keeps the backward pass's inputs, where there is to be one, in 8 bits.  Weights are trained if `trainable`."""
 
     def __init__(self, d: int, post_norm: bool = False, gate: bool = False, scale: float = 1.0, eps: float = 1e-5, checkpoint: bool = True, trainable: bool = False,
                  dtype=torch.bfloat16, device="cuda"):
@@ -120,9 +121,10 @@ class BlockNorm(torch.nn.Module):
         self.scale, self.eps, self.checkpoint = scale, eps, checkpoint
 
     def forward(self, x: torch.Tensor, branch: Optional[torch.Tensor] = None):
+        keeps = self.checkpoint and torch.is_grad_enabled()
         if branch is None:
-            return x, _NormFn.apply(x, None, self.weight, None, None, 1.0, self.eps, self.checkpoint)[0]
-        return _NormFn.apply(x, branch, self.weight, self.post_weight, self.gate, self.scale, self.eps, self.checkpoint)[:2]
+            return x, _NormFn.apply(x, None, self.weight, None, None, 1.0, self.eps, keeps)[0]
+        return _NormFn.apply(x, branch, self.weight, self.post_weight, self.gate, self.scale, self.eps, keeps)[:2]
 
 
 class _SwigluFn(torch.autograd.Function):
@@ -130,6 +132,7 @@ class _SwigluFn(torch.autograd.Function):
     def forward(ctx, g, u, checkpoint):
         g2, u2 = _rows(g), _rows(u)
         T, m = g2.shape
+        checkpoint = checkpoint and any(ctx.needs_input_grad)
         h = torch.empty(T, m, dtype=g.dtype, device=g.device)
         gq = g_exp = uq = u_exp = None
         if checkpoint:
@@ -150,7 +153,7 @@ class _SwigluFn(torch.autograd.Function):
 
 def swiglu(g: torch.Tensor, u: torch.Tensor, checkpoint: bool = True) -> torch.Tensor:
     """silu(g) * u; with `checkpoint`, g and u are kept for the backward pass in 8 bits."""
-    return _SwigluFn.apply(g, u, checkpoint)[0]
+    return _SwigluFn.apply(g, u, checkpoint and torch.is_grad_enabled())[0]
 
 
 class _TokenLogprobFn(torch.autograd.Function):

@@ -159,3 +159,20 @@ def test_loss_under_another_default_type(calls):
     finally:
         torch.set_default_dtype(kept)
     assert loss.dtype == rewards.dtype == torch.float32
+
+
+# ---- checkpoints ------------------------------------------------------------------------------------------------------------------
+def test_checkpoints_are_written_where_a_backward_pass_reads_them(calls):
+    n = norm(32, post_norm=True)
+    x, y = torch.randn(3, 32), torch.randn(3, 32)
+    run = lambda x, y: (n(x, y), n(x), block.swiglu(x, y), [a[1] for a in calls.asked if a[0].endswith("fwd")], calls.asked.clear())[3]  # noqa: E731
+    assert run(x.requires_grad_(), y) == [True, True, True]
+    assert run(x, y.requires_grad_()) == [True, True, True]
+    assert run(x.detach(), y) == [True, False, True]                            # what depends on y
+    assert run(x.detach(), y.detach()) == [False, False, False]                 # no input needs a gradient
+    with torch.no_grad():
+        assert run(x, y) == [False, False, False]
+    with torch.inference_mode():
+        assert run(x, y) == [False, False, False]
+    n.weight.requires_grad_()
+    assert run(x.detach(), y.detach()) == [True, True, False]                   # a norm's weight is trained
