@@ -160,7 +160,8 @@ class _TokenLogprobFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels):
         x = logits.reshape(-1, logits.shape[-1])
-        x = x if x.shape[1] == 1 or x.stride(1) == 1 else x.contiguous()
+        apart = (x.shape[1] == 1 or x.stride(1) == 1) and (x.shape[0] == 1 or x.stride(0) >= x.shape[1])
+        x = x if apart else x.contiguous()
         T, V = x.shape
         logp, lse, low = (torch.empty(T, dtype=torch.float32, device=x.device) for _ in range(3))
         l2 = labels.reshape(-1).contiguous()

@@ -176,3 +176,19 @@ def test_checkpoints_are_written_where_a_backward_pass_reads_them(calls):
         assert run(x, y) == [False, False, False]
     n.weight.requires_grad_()
     assert run(x.detach(), y.detach()) == [True, True, False]                   # a norm's weight is trained
+
+
+# ---- shapes and memory ------------------------------------------------------------------------------------------------------------
+def test_logits_whose_rows_lie_over_each_other(calls):
+    row = torch.randn(1, 9)
+    x = row.expand(4, 9)                                                        # one row four times, without memory of its own
+    labels = torch.tensor([0, 3, 8, -100])
+    want = torch.log_softmax(row, 1)[0, labels.clamp(min=0)] * (labels >= 0)
+    assert torch.allclose(block.token_logprobs(x, labels), want)
+    row.requires_grad_()
+    block.token_logprobs(row.expand(4, 9), torch.tensor([0, 3, 8, 1])).sum().backward()
+    want = -4 * torch.softmax(row.detach(), 1)
+    want[0, [0, 3, 8, 1]] += 1.0
+    assert torch.allclose(row.grad, want, atol=1e-6)
+    sliding = torch.randn(12).unfold(0, 9, 1)                                   # rows one element apart
+    assert torch.allclose(block.token_logprobs(sliding, labels), torch.log_softmax(sliding, 1).gather(1, labels.clamp(min=0)[:, None])[:, 0] * (labels >= 0))
