@@ -20,11 +20,15 @@ _U8 = torch.uint8
 def _rows(t: torch.Tensor) -> torch.Tensor:
     """[..., n] as [T, n] whose rows may lie apart, as the kernels take them."""
     t2 = t.reshape(-1, t.shape[-1])
-    by = 16
     ok = t2.shape[1] == 1 or t2.stride(1) == 1
     if t2.shape[0] > 1:
-        ok = ok and t2.stride(0) >= t2.shape[1] and t2.stride(0) % by == 0
-    return t2 if ok and t2.data_ptr() % 16 == 0 else t2.contiguous()
+        ok = ok and t2.stride(0) >= t2.shape[1] and t2.stride(0) % 16 == 0
+    return t2 if ok and t2.data_ptr() % 16 == 0 else t2.clone(memory_format=torch.contiguous_format)     # also of a dense one that begins elsewhere
+
+
+def _dense_bf16(t: torch.Tensor, width: int) -> torch.Tensor:
+    t2 = t.reshape(-1, width).to(torch.bfloat16).contiguous()
+    return t2 if t2.data_ptr() % 16 == 0 else t2.clone()
 
 
 def _codes(T: int, n: int, dev) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -231,7 +235,7 @@ class _Mx4Fn(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, *layers):
-        x2 = x.reshape(-1, x.shape[-1]).to(torch.bfloat16).contiguous()
+        x2 = _dense_bf16(x, x.shape[-1])
         outs, codes = [], None
         for l in layers:
             y, codes = _mx4_product(x2, l.wq, l.w_exp, l.out_features, codes)
@@ -252,7 +256,7 @@ class _Mx4Fn(torch.autograd.Function):
                 continue
             if l.wtq is None:
                 raise RuntimeError("this layer was built without input_grad=True, so it holds no codes of its transposed weight")
-            dx, _ = _mx4_product(dy.reshape(-1, l.out_features).to(torch.bfloat16).contiguous(), l.wtq, l.wt_exp, l.in_features)
+            dx, _ = _mx4_product(_dense_bf16(dy, l.out_features), l.wtq, l.wt_exp, l.in_features)
             total = dx if total is None else total.add_(dx)
         return (None if total is None else total.to(ctx.dtype).reshape(ctx.shape),) + (None,) * len(ctx.layers)
 

@@ -192,3 +192,30 @@ def test_logits_whose_rows_lie_over_each_other(calls):
     assert torch.allclose(row.grad, want, atol=1e-6)
     sliding = torch.randn(12).unfold(0, 9, 1)                                   # rows one element apart
     assert torch.allclose(block.token_logprobs(sliding, labels), torch.log_softmax(sliding, 1).gather(1, labels.clamp(min=0)[:, None])[:, 0] * (labels >= 0))
+
+
+def test_dense_inputs_off_the_16_byte_boundaries(calls, monkeypatch):
+    """A dense view that begins anywhere is copied: contiguous() would hand back the same memory."""
+    flat = torch.randn(2, 1 + 3 * 32)
+    g, u = (f[1:].view(3, 32) for f in flat)
+    if g.data_ptr() % 16 == 0:
+        g, u = (f[:-1].view(3, 32) for f in flat)
+    assert g.is_contiguous() and g.data_ptr() % 16
+    out = block.swiglu(g, u)
+    assert calls.asked[-1][2] and torch.allclose(out, torch.nn.functional.silu(g) * u, atol=1e-6)
+    seen = []
+    monkeypatch.setattr(block, "_mx4_product", lambda x2, wq, w_exp, m, codes=None: (seen.append(x2), (torch.ones(3, m, dtype=torch.bfloat16), None))[1])
+    layer = first_layer()
+    half = torch.randn(1 + 3 * 32).bfloat16()[1:].view(3, 32).requires_grad_()
+    assert half.data_ptr() % 16
+    y = layer(half)
+    y.backward(torch.randn(1 + 3 * 16).bfloat16()[1:].view(3, 16))
+    assert len(seen) == 2 and all(t.is_contiguous() and t.data_ptr() % 16 == 0 for t in seen) and torch.equal(seen[0], half)
+
+
+def first_layer():
+    layer = block.Mx4Linear.__new__(block.Mx4Linear)
+    torch.nn.Module.__init__(layer)
+    layer.in_features, layer.out_features = 32, 16
+    layer.wq, layer.w_exp, layer.wtq, layer.wt_exp = (torch.zeros(1) for _ in range(4))
+    return layer
