@@ -31,6 +31,14 @@ def _dense_bf16(t: torch.Tensor, width: int) -> torch.Tensor:
     return t2 if t2.data_ptr() % 16 == 0 else t2.clone()
 
 
+def _check_rows(a, b, what: str) -> None:
+    """Leading shapes that name the same rows in the same order: alike up to ones in front, or one of them flat."""
+    short, long = sorted((tuple(a), tuple(b)), key=len)
+    alike = (1,) * (len(long) - len(short)) + short == long
+    if not alike and not (min(len(a), len(b)) <= 1 and torch.Size(a).numel() == torch.Size(b).numel()):
+        raise ValueError(f"{what}: rows of shapes {tuple(a)} and {tuple(b)}")
+
+
 def _codes(T: int, n: int, dev) -> Tuple[torch.Tensor, torch.Tensor]:
     return torch.empty(T, n, dtype=_U8, device=dev), torch.empty(T, (n + 31) // 32, dtype=_U8, device=dev)
 
@@ -69,6 +77,8 @@ class _NormFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, b, w, w_post, gate, scale, eps, checkpoint):
         ctx.set_materialize_grads(False)
+        if b is not None:
+            _check_rows(x.shape[:-1], b.shape[:-1], "stream and branch")
         x2, b2 = _rows(x), None if b is None else _rows(b)
         T, d, dev, dt = x2.shape[0], x2.shape[1], x.device, x.dtype
         checkpoint = checkpoint and any(ctx.needs_input_grad)
@@ -85,14 +95,14 @@ class _NormFn(torch.autograd.Function):
         saved_s = sq if checkpoint else x2 if s is None else s
         saved_b = None if not reads_b else bq if checkpoint else b2
         ctx.save_for_backward(saved_s, s_exp, saved_b, b_exp, rstd, rstd_b, w, w_post, gate, tie := _tie(x))
-        ctx.scale, ctx.shape, ctx.branch = scale, x.shape, b is not None
+        ctx.scale, ctx.shape, ctx.branch = scale, x.shape, None if b is None else b.shape
         h = h.reshape(x.shape)
         return (h, tie) if s is None else (s.reshape(x.shape), h, tie)
 
     @staticmethod
     @_first_order
     def backward(ctx, *grads):
-        ds, dh = (None, grads[0]) if not ctx.branch else grads
+        ds, dh = (None, grads[0]) if ctx.branch is None else grads
         s, s_exp, b, b_exp, rstd, rstd_b, w, w_post, gate, _ = ctx.saved_tensors
         T, d, dev = s.shape[0], s.shape[1], s.device
         dh2 = torch.zeros(T, d, dtype=w.dtype, device=dev) if dh is None else _rows(dh)
@@ -106,7 +116,7 @@ class _NormFn(torch.autograd.Function):
         _b.norm_bwd(dh2, s, w, rstd, dx, ds=ds2, b=b, db=db, scale=ctx.scale, gate=gate, w_post=w_post, rstd_b=rstd_b, s_exp=s_exp, b_exp=b_exp, dw=dw,
                     dw_post=dw_post, dgate=dgate, ws=ws)
         of = lambda v, p: None if v is None else v.to(p.dtype)  # noqa: E731
-        return (dx.reshape(ctx.shape), None if db is None else db.reshape(ctx.shape), of(dw, w), of(dw_post, w_post), of(dgate, gate), None, None, None)
+        return (dx.reshape(ctx.shape), None if db is None else db.reshape(ctx.branch), of(dw, w), of(dw_post, w_post), of(dgate, gate), None, None, None)
 
 
 class BlockNorm(torch.nn.Module):
@@ -134,6 +144,7 @@ class BlockNorm(torch.nn.Module):
 class _SwigluFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, g, u, checkpoint):
+        _check_rows(g.shape[:-1], u.shape[:-1], "gate and up")
         g2, u2 = _rows(g), _rows(u)
         T, m = g2.shape
         checkpoint = checkpoint and any(ctx.needs_input_grad)
@@ -143,6 +154,7 @@ class _SwigluFn(torch.autograd.Function):
             (gq, g_exp), (uq, u_exp) = _codes(T, m, g.device), _codes(T, m, g.device)
         _b.swiglu_fwd(g2, u2, h, gq=gq, g_exp=g_exp, uq=uq, u_exp=u_exp)
         ctx.save_for_backward(gq if checkpoint else g2, uq if checkpoint else u2, g_exp, u_exp, tie := _tie(g))
+        ctx.up = u.shape
         return h.reshape(g.shape), tie
 
     @staticmethod
@@ -152,7 +164,7 @@ class _SwigluFn(torch.autograd.Function):
         dh2 = _rows(dh)
         dg, du = (torch.empty(dh2.shape, dtype=dh.dtype, device=dh.device) for _ in range(2))
         _b.swiglu_bwd(dh2, g, u, dg, du, g_exp=g_exp, u_exp=u_exp)
-        return dg.reshape(dh.shape), du.reshape(dh.shape), None
+        return dg.reshape(dh.shape), du.reshape(ctx.up), None
 
 
 def swiglu(g: torch.Tensor, u: torch.Tensor, checkpoint: bool = True) -> torch.Tensor:
@@ -163,6 +175,7 @@ def swiglu(g: torch.Tensor, u: torch.Tensor, checkpoint: bool = True) -> torch.T
 class _TokenLogprobFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels):
+        _check_rows(logits.shape[:-1], labels.shape, "logits and labels")
         x = logits.reshape(-1, logits.shape[-1])
         apart = (x.shape[1] == 1 or x.stride(1) == 1) and (x.shape[0] == 1 or x.stride(0) >= x.shape[1])
         x = x if apart else x.contiguous()

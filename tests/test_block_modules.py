@@ -219,3 +219,34 @@ def first_layer():
     layer.in_features, layer.out_features = 32, 16
     layer.wq, layer.w_exp, layer.wtq, layer.wt_exp = (torch.zeros(1) for _ in range(4))
     return layer
+
+
+@pytest.mark.parametrize("x,y", [((2, 3, 32), (3, 2, 32)), ((2, 1, 32), (1, 2, 32)), ((4, 32), (2, 2, 2, 16)), ((2, 2, 3, 32), (4, 3, 32))])
+def test_inputs_of_different_shapes_are_refused(calls, x, y):
+    """As many rows in another order are not the same rows."""
+    a, b = torch.randn(x), torch.randn(y)
+    with pytest.raises(ValueError):
+        norm(32)(a, b)
+    with pytest.raises(ValueError):
+        block.swiglu(a, b)
+    if y[-1] == 32:
+        with pytest.raises(ValueError):
+            block.token_logprobs(a, torch.zeros(y[:-1], dtype=torch.int64))
+
+
+@pytest.mark.parametrize("x,y", [((2, 3, 32), (2, 3, 32)), ((1, 6, 32), (6, 32)), ((6, 32), (1, 1, 6, 32)), ((2, 3, 32), (6, 32)), ((6, 32), (2, 3, 32))])
+def test_leading_ones_and_flat_rows_are_taken(calls, x, y):
+    """The results have the first one's shape, every gradient that of its own input."""
+    a, b = torch.randn(x, requires_grad=True), torch.randn(y, requires_grad=True)
+    s, h = norm(32, checkpoint=False)(a, b)
+    z = block.swiglu(a, b, checkpoint=False)
+    assert s.shape == h.shape == z.shape == a.shape
+    (s.sum() + h.square().sum() + z.sum()).backward()
+    assert a.grad.shape == a.shape and b.grad.shape == b.shape
+    a64, b64 = a.detach().double().requires_grad_(), b.detach().double().requires_grad_()
+    s64 = a64.reshape(6, 32) + b64.reshape(6, 32)
+    h64 = s64 * (s64.square().mean(1, keepdim=True) + 1e-5).rsqrt()
+    (s64.sum() + h64.square().sum() + (torch.nn.functional.silu(a64.reshape(6, 32)) * b64.reshape(6, 32)).sum()).backward()
+    assert torch.allclose(a.grad.double(), a64.grad, atol=1e-5) and torch.allclose(b.grad.double(), b64.grad, atol=1e-5)
+    labels = torch.arange(6).reshape(y[:-1])
+    assert torch.allclose(block.token_logprobs(a, labels).reshape(-1), torch.log_softmax(a.reshape(6, 32), 1)[torch.arange(6), torch.arange(6)], atol=1e-5)
