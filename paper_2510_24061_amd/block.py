@@ -378,6 +378,8 @@ def preference_step(policy, reference, tokens: torch.Tensor, prompt_lengths: tor
     """Loss and rewards of pairs: tokens [2 P, S] (chosen answers first, rows filled up with anything), of which row i has `lengths[i]`, the first
     `prompt_lengths[i]` its prompt's.  Call backward() on the loss, then an optimizer."""
     labels = _next_labels(tokens, prompt_lengths, lengths)
+    inside = torch.arange(tokens.shape[1], device=tokens.device) < lengths[:, None]
+    tokens = torch.where(inside, tokens, torch.zeros_like(tokens))              # an embedding looks up what rows are filled up with, too
     with torch.no_grad():
         ref = token_logprobs(reference(tokens), labels)
     logp = token_logprobs(policy(tokens), labels)

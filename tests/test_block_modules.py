@@ -250,3 +250,19 @@ def test_leading_ones_and_flat_rows_are_taken(calls, x, y):
     assert torch.allclose(a.grad.double(), a64.grad, atol=1e-5) and torch.allclose(b.grad.double(), b64.grad, atol=1e-5)
     labels = torch.arange(6).reshape(y[:-1])
     assert torch.allclose(block.token_logprobs(a, labels).reshape(-1), torch.log_softmax(a.reshape(6, 32), 1)[torch.arange(6), torch.arange(6)], atol=1e-5)
+
+
+# ---- the preference step -----------------------------------------------------------------------------------------------------------
+def test_what_rows_are_filled_up_with_reaches_no_embedding(calls):
+    """Rows may be filled up with anything: -100, or ids beyond the vocabulary."""
+    V, d = 11, 8
+    embedding, head = torch.randn(V, d), torch.randn(V, d)
+    model = lambda tokens: torch.nn.functional.embedding(tokens, embedding).cumsum(1) @ head.t()  # noqa: E731
+    g = torch.Generator().manual_seed(0)
+    tokens = torch.randint(0, V, (4, 9), generator=g)
+    prompts, lengths = torch.tensor([2, 0, 2, 1]), torch.tensor([9, 5, 1, 7])
+    plain = block.preference_step(model, model, tokens, prompts, lengths)
+    filled = torch.where(torch.arange(9) < lengths[:, None], tokens, torch.tensor([-100, 10 ** 6, -1, V])[:, None])
+    kept = filled.clone()
+    loss, rewards = block.preference_step(model, model, filled, prompts, lengths)
+    assert torch.equal(loss, plain[0]) and torch.equal(rewards, plain[1]) and torch.equal(filled, kept)
