@@ -395,7 +395,8 @@ falqon_status falqon_svd_right_factor(const float* e, int64_t m, int64_t n, int6
  *   x     in   [rows, cols] of dtype xt, row stride ld_x elements (a multiple of 16)
  *   q     out  E4M3: [rows, cols] bytes.  E2M1: [rows, cols / 2] bytes, the even column in the low half
  *   exps  out  E4M3: [rows, ceil(cols / 32)].  E2M1: [rows, falqon_mx4_exp_pitch(cols)], behind the last block zeros
- * cols is a multiple of 16 (E4M3) or 32 (E2M1); rows >= 0.  falqon_mx_dequantize writes the values in dtype xt, exactly in bf16
+ * cols is a multiple of 16 (E4M3) or 32 (E2M1), at most 2^20; 0 <= rows <= 2^24, and rows * cols, a row's last block counted whole, is below
+ * 2^35 (bf16) or 2^34 (fp32), which is what a launch takes.  falqon_mx_dequantize writes the values in dtype xt, exactly in bf16
  * and fp32 (but for values below their range).
  */
 typedef enum { FALQON_MX_E4M3 = 0, FALQON_MX_E2M1 = 1 } falqon_mx_fmt;
@@ -412,7 +413,7 @@ falqon_status falqon_mx_dequantize(const uint8_t* q, const uint8_t* exps, falqon
  *   wq, w_exp   in      E2M1 codes [m, n / 2] and exponents [m, falqon_mx4_exp_pitch(n)] of the weight
  *   xq, x_exp   in/out  E2M1 codes [T, n / 2] and exponents [T, falqon_mx4_exp_pitch(n)]: out when x is given
  *   y           out     [T, m] of dtype yt
- * n is a multiple of 32, m of 16, T >= 1.  Its input gradient is the same call on the output gradient and the codes of the transposed
+ * n is a multiple of 32, m of 16, at most 2^20; 1 <= T <= 2^24; x is bounded as in falqon_mx_quantize, y by less than 2^24 tiles of 256 x 256.  Its input gradient is the same call on the output gradient and the codes of the transposed
  * weight.  y may not lie over an input.
  */
 falqon_status falqon_mx4_linear(const void* x, const uint8_t* wq, const uint8_t* w_exp, int64_t T, int64_t n, int64_t m,
@@ -430,7 +431,8 @@ falqon_status falqon_mx4_linear(const void* x, const uint8_t* wq, const uint8_t*
  *   s                 out  [T, d]; needed where b is given, not written otherwise; it may lie over x or b where these are dense
  *   rstd, rstd_b      out  fp32 [T]; rstd_b where w_post is given
  *   sq, s_exp         out  nullable: s as an 8-bit checkpoint (falqon_mx_quantize, E4M3);  bq, b_exp the same of b
- * d is a multiple of 16, at most 16384; T >= 1.
+ * d is a multiple of 16, at most 16384; 1 <= T <= 2^24, and the launch takes T * d < 2^35 (bf16) or 2^34 (fp32), less for a width between
+ * whole waves.
  */
 typedef struct falqon_norm_fwd_args {
     const void *x, *b, *w, *w_post, *gate;
@@ -480,7 +482,8 @@ falqon_status falqon_norm_bwd(const falqon_norm_bwd_args* args, void* stream);
  *   h      out  [T, m];  it may lie over g or u where these are dense
  *   gq, g_exp, uq, u_exp  out, nullable together
  * Backward: dh in [T, m] with row stride ld_dh; g, u with g_exp and u_exp NULL as they are (row strides ld_g, ld_u), else dense codes;
- * dg, du out [T, m], either may lie over dense dh, g or u of dtype xt.  m is a multiple of 16; T >= 1.
+ * dg, du out [T, m], either may lie over dense dh, g or u of dtype xt.  m is a multiple of 16, at most 2^20; T >= 1; T and T * m
+ * are bounded as in falqon_mx_quantize.
  */
 falqon_status falqon_swiglu_fwd(const void* g, const void* u, falqon_dtype xt, int64_t T, int64_t m, int64_t ld_g, int64_t ld_u,
                                 void* h, uint8_t* gq, uint8_t* g_exp, uint8_t* uq, uint8_t* u_exp, void* stream);
@@ -495,7 +498,7 @@ falqon_status falqon_swiglu_bwd(const void* dh, int64_t ld_dh, const void* g, co
  *
  * A token whose label is outside [0, V) (-100, say) does not count: its logits are not read, logp = lse = 0, dx = 0.  Logits of
  * -infinity have probability 0; a row of nothing else has lse = logp = -infinity and dx = 0.  A row that holds +infinity or NaN gives NaN.
- *   logits    in   [T, V] of dtype lt, row stride ld elements; any V >= 1, any stride >= V, aligned to the element
+ *   logits    in   [T, V] of dtype lt, row stride ld elements; 1 <= T < 2^24, 1 <= V <= 2^20, any stride >= V, aligned to the element
  *   labels    in   int64 [T]
  *   logp, lse out  fp32 [T]
  *   dlogits   out  [T, V] of dtype lt, row stride ld_d; it may be the logits themselves
@@ -526,7 +529,7 @@ falqon_status falqon_token_logprob_bwd_low(const float* d_logp, const void* logi
  *   logp, ref_logp  in  fp32 [T], 0 for tokens that do not count.  A logp of -infinity (a masked label) makes its reward -infinity and the pair's loss
  *             infinite, or without smoothing 0 where it is the rejected one's; a reward without a value (both -infinity) makes the loss NaN
  *   loss, rewards, d_logp  out  fp32 [1], [2, P], [T]
- * 0 <= smoothing < 0.5, beta finite; 1 <= P <= 65536.  ws: falqon_logprob_workspace_bytes(T, 1, P) bytes.
+ * 0 <= smoothing < 0.5, beta finite; 1 <= T <= 2^24; 1 <= P <= 65536.  ws: falqon_logprob_workspace_bytes(T, 1, P) bytes.
  */
 falqon_status falqon_preference_loss(const float* logp, const float* ref_logp, const int64_t* offsets, int64_t T, int64_t P, double beta,
                                      double smoothing, float* loss, float* rewards, float* d_logp, void* ws, size_t ws_bytes, void* stream);

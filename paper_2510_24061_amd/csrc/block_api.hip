@@ -19,6 +19,10 @@ bool any_odd(unsigned by, P... p) { return ((reinterpret_cast<uintptr_t>(p) | ..
 bool bad_type(falqon_dtype t) { return t != FALQON_BF16 && t != FALQON_F32; }
 bool bad_matrix(int64_t rows, int64_t cols, int64_t by) { return rows < 1 || rows > kMaxRows || cols < by || cols > kMaxWidth || cols % by; }
 bool bad_stride(int64_t ld, int64_t cols) { return ld < cols || ld % 16 || ld > (int64_t(1) << 32); }
+// What a launch takes along a dimension: fewer than 2^32 threads.
+bool too_many(int64_t blocks, int64_t threads) { return blocks > ((int64_t(1) << 32) - 1) / threads; }
+// the passes of one 16-byte piece a lane (mx_common.h), in which a row's last block of 32 columns counts whole
+bool too_many_pieces(int64_t rows, int64_t cols, falqon_dtype t) { return too_many((rows * ((cols + 31) / 32 * (t == FALQON_F32 ? 8 : 4)) + 255) / 256, 256); }
 falqon_status status_of(hipError_t e) { return e == hipSuccess ? FALQON_OK : FALQON_ERR_HIP; }
 hipStream_t on(void* stream) { return static_cast<hipStream_t>(stream); }
 
@@ -31,17 +35,17 @@ extern "C" {
 
 int64_t falqon_mx4_exp_pitch(int64_t cols) { return cols < 32 || cols % 32 ? 0 : (cols + 511) / 512 * 16; }
 
-static bool bad_mx(int64_t rows, int64_t cols, int64_t ld, falqon_mx_fmt fmt)
+static bool bad_mx(int64_t rows, int64_t cols, int64_t ld, falqon_mx_fmt fmt, falqon_dtype t)
 {
     return rows < 0 || rows > kMaxRows || cols < 16 || cols > kMaxWidth || cols % (fmt == FALQON_MX_E2M1 ? 32 : 16) || rows * cols > kMaxElements ||
-           bad_stride(ld, cols);
+           too_many_pieces(rows, cols, t) || bad_stride(ld, cols);
 }
 
 falqon_status falqon_mx_quantize(const void* x, falqon_dtype xt, int64_t rows, int64_t cols, int64_t ld_x, falqon_mx_fmt fmt,
                                  uint8_t* q, uint8_t* exps, void* stream)
 {
     if (bad_type(xt) || (fmt != FALQON_MX_E4M3 && fmt != FALQON_MX_E2M1)) return FALQON_ERR_ENUM;
-    if (bad_mx(rows, cols, ld_x, fmt)) return FALQON_ERR_SHAPE;
+    if (bad_mx(rows, cols, ld_x, fmt, xt)) return FALQON_ERR_SHAPE;
     if (rows == 0) return FALQON_OK;
     if (!x || !q || !exps) return FALQON_ERR_NULL;
     if (any_misaligned(x, q, exps)) return FALQON_ERR_ALIGN;
@@ -52,7 +56,7 @@ falqon_status falqon_mx_dequantize(const uint8_t* q, const uint8_t* exps, falqon
                                    void* x, falqon_dtype xt, int64_t ld_x, void* stream)
 {
     if (bad_type(xt) || (fmt != FALQON_MX_E4M3 && fmt != FALQON_MX_E2M1)) return FALQON_ERR_ENUM;
-    if (bad_mx(rows, cols, ld_x, fmt)) return FALQON_ERR_SHAPE;
+    if (bad_mx(rows, cols, ld_x, fmt, xt)) return FALQON_ERR_SHAPE;
     if (rows == 0) return FALQON_OK;
     if (!x || !q || !exps) return FALQON_ERR_NULL;
     if (any_misaligned(x, q, exps)) return FALQON_ERR_ALIGN;
@@ -63,7 +67,9 @@ falqon_status falqon_mx4_linear(const void* x, const uint8_t* wq, const uint8_t*
                                 uint8_t* xq, uint8_t* x_exp, void* y, falqon_dtype yt, void* stream)
 {
     if (bad_type(yt)) return FALQON_ERR_ENUM;
-    if (bad_matrix(T, n, 32) || bad_matrix(T, m, 16) || T * n > kMaxElements) return FALQON_ERR_SHAPE;
+    if (bad_matrix(T, n, 32) || bad_matrix(T, m, 16) || T * n > kMaxElements || T * m > kMaxElements ||
+        too_many(((T + 255) / 256 * ((m + 255) / 256) + 7) / 8 * 8, 256) || (x && too_many_pieces(T, n, FALQON_BF16)))
+        return FALQON_ERR_SHAPE;
     if (!wq || !w_exp || !xq || !x_exp || !y) return FALQON_ERR_NULL;
     if (any_misaligned(x, wq, w_exp, xq, x_exp, y)) return FALQON_ERR_ALIGN;
     const Mx4Gemm product{xq, x_exp, wq, w_exp, T, m, n, y, yt == FALQON_F32};
@@ -80,7 +86,7 @@ falqon_status falqon_norm_fwd(const falqon_norm_fwd_args* a, void* stream)
     if (!a) return FALQON_ERR_NULL;
     if (bad_type(a->xt)) return FALQON_ERR_ENUM;
     if (bad_matrix(a->T, a->d, 16) || a->d > kNormMaxWidth || bad_stride(a->ld_x, a->d) || (a->b && bad_stride(a->ld_b, a->d)) ||
-        !std::isfinite(a->scale) || !(a->eps >= 0.0))
+        !std::isfinite(a->scale) || !(a->eps >= 0.0) || norm_fwd_threads(a->T, a->d, a->xt == FALQON_F32) >= int64_t(1) << 32)
         return FALQON_ERR_SHAPE;
     if (!a->x || !a->w || !a->h || !a->rstd || (!a->b && (a->w_post || a->gate || a->bq)) || (a->b && !a->s) || (a->w_post && !a->rstd_b) ||
         !a->sq != !a->s_exp || !a->bq != !a->b_exp)
@@ -120,7 +126,7 @@ falqon_status falqon_swiglu_fwd(const void* g, const void* u, falqon_dtype xt, i
                                 void* h, uint8_t* gq, uint8_t* g_exp, uint8_t* uq, uint8_t* u_exp, void* stream)
 {
     if (bad_type(xt)) return FALQON_ERR_ENUM;
-    if (bad_matrix(T, m, 16) || T * m > kMaxElements || bad_stride(ld_g, m) || bad_stride(ld_u, m)) return FALQON_ERR_SHAPE;
+    if (bad_matrix(T, m, 16) || T * m > kMaxElements || too_many_pieces(T, m, xt) || bad_stride(ld_g, m) || bad_stride(ld_u, m)) return FALQON_ERR_SHAPE;
     if (!g || !u || !h || !gq != !g_exp || !gq != !uq || !gq != !u_exp) return FALQON_ERR_NULL;
     if (any_misaligned(g, u, h, gq, uq)) return FALQON_ERR_ALIGN;
     return status_of(launch_swiglu_fwd(SwigluFwd{g, u, ld_g, ld_u, T, m, h, gq, g_exp, uq, u_exp}, xt == FALQON_F32, on(stream)));
@@ -130,7 +136,9 @@ falqon_status falqon_swiglu_bwd(const void* dh, int64_t ld_dh, const void* g, co
                                 int64_t ld_g, int64_t ld_u, falqon_dtype xt, int64_t T, int64_t m, void* dg, void* du, void* stream)
 {
     if (bad_type(xt)) return FALQON_ERR_ENUM;
-    if (bad_matrix(T, m, 16) || T * m > kMaxElements || bad_stride(ld_dh, m) || (!g_exp && (bad_stride(ld_g, m) || bad_stride(ld_u, m)))) return FALQON_ERR_SHAPE;
+    if (bad_matrix(T, m, 16) || T * m > kMaxElements || too_many_pieces(T, m, xt) || bad_stride(ld_dh, m) ||
+        (!g_exp && (bad_stride(ld_g, m) || bad_stride(ld_u, m))))
+        return FALQON_ERR_SHAPE;
     if (!dh || !g || !u || !dg || !du || !g_exp != !u_exp) return FALQON_ERR_NULL;
     if (any_misaligned(dh, g, u, dg, du)) return FALQON_ERR_ALIGN;
     return status_of(launch_swiglu_bwd(SwigluBwd{dh, ld_dh, g, u, ld_g, ld_u, g_exp, u_exp, T, m, dg, du}, xt == FALQON_F32, on(stream)));
@@ -157,7 +165,7 @@ falqon_status falqon_token_logprob_low(const void* logits, falqon_dtype lt, int6
                                        float* logp, float* lse, float* lse_low, void* ws, size_t ws_bytes, void* stream)
 {
     if (bad_type(lt)) return FALQON_ERR_ENUM;
-    if (bad_logits(T, V) || ld < V) return FALQON_ERR_SHAPE;
+    if (bad_logits(T, V) || ld < V || too_many(T, 256)) return FALQON_ERR_SHAPE;
     if (!logits || !labels || !logp || !lse) return FALQON_ERR_NULL;
     if (any_odd(lt == FALQON_F32 ? 4 : 2, logits) || any_odd(8, labels) || any_odd(4, logp, lse, lse_low) || any_misaligned(ws)) return FALQON_ERR_ALIGN;
     if (!ws || ws_bytes < falqon_logprob_workspace_bytes(T, V, 1)) return FALQON_ERR_WORKSPACE;
@@ -174,7 +182,7 @@ falqon_status falqon_token_logprob_bwd_low(const float* d_logp, const void* logi
                                            const int64_t* labels, const float* lse, const float* lse_low, void* dlogits, int64_t ld_d, void* stream)
 {
     if (bad_type(lt)) return FALQON_ERR_ENUM;
-    if (bad_logits(T, V) || ld < V || ld_d < V || (logits == dlogits && ld != ld_d)) return FALQON_ERR_SHAPE;
+    if (bad_logits(T, V) || too_many(T, 256) || ld < V || ld_d < V || (logits == dlogits && ld != ld_d)) return FALQON_ERR_SHAPE;
     if (!d_logp || !logits || !labels || !lse || !dlogits) return FALQON_ERR_NULL;
     if (any_odd(lt == FALQON_F32 ? 4 : 2, logits, dlogits) || any_odd(8, labels) || any_odd(4, d_logp, lse, lse_low)) return FALQON_ERR_ALIGN;
     return status_of(launch_token_logprob_bwd(TokenLogprobBwd{d_logp, logits, ld, labels, lse, lse_low, T, V, dlogits, ld_d}, lt == FALQON_F32, on(stream)));

@@ -15,6 +15,7 @@ struct NormFwd {
     float *rstd, *rstd_b;
     uint8_t *sq, *s_exp, *bq, *b_exp;
 };
+int64_t norm_fwd_threads(int64_t T, int64_t d, bool f32);   // of its launch
 hipError_t launch_norm_fwd(const NormFwd& a, bool f32, hipStream_t stream);
 
 struct NormBwd {

@@ -386,14 +386,22 @@ norm_sum_kernel(const float* __restrict__ partial, int parts, const NormBwd a)
     if (a.dw_post) a.dw_post[column] = a.gate ? sum * element(static_cast<const T*>(a.gate) + column) : sum;
 }
 
+struct FwdShape { int P, waves, rows; };                              // pieces a lane, waves a row, rows a workgroup
+template <typename T>
+FwdShape fwd_shape(int64_t d)
+{
+    constexpr int E = kPiece<T>;
+    const int pieces = static_cast<int>(d) / E;
+    int P = 1, waves = (pieces + 63) / 64;
+    while (waves > 4 && P < 16 / E) { P *= 2; waves = (pieces + 64 * P - 1) / (64 * P); }
+    return {P, waves, waves >= 4 ? 1 : 4 / waves};
+}
+
 template <typename T, bool POST>
 void run_fwd(const NormFwd& a, hipStream_t stream)
 {
     constexpr int E = kPiece<T>;
-    const int pieces = static_cast<int>(a.d) / E;
-    int P = 1, waves = (pieces + 63) / 64;
-    while (waves > 4 && P < 16 / E) { P *= 2; waves = (pieces + 64 * P - 1) / (64 * P); }
-    const int rows = waves >= 4 ? 1 : 4 / waves;
+    const auto [P, waves, rows] = fwd_shape<T>(a.d);
     const unsigned grid = static_cast<unsigned>((a.T + rows - 1) / rows);
     const int threads = 64 * waves * rows;
     if (P == 1) norm_fwd_kernel<T, 1, POST><<<grid, threads, 0, stream>>>(a, waves, rows);
@@ -439,6 +447,12 @@ void bwd_by_mode(const NormBwd& a, float* partial, hipStream_t stream)
 }
 
 }  // namespace
+
+int64_t norm_fwd_threads(int64_t T, int64_t d, bool f32)
+{
+    const FwdShape s = f32 ? fwd_shape<float>(d) : fwd_shape<uint16_t>(d);
+    return (T + s.rows - 1) / s.rows * (64 * s.waves * s.rows);
+}
 
 hipError_t launch_norm_fwd(const NormFwd& a, bool f32, hipStream_t stream)
 {
