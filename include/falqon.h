@@ -432,7 +432,7 @@ falqon_status falqon_mx4_linear(const void* x, const uint8_t* wq, const uint8_t*
  *   rstd, rstd_b      out  fp32 [T]; rstd_b where w_post is given
  *   sq, s_exp         out  nullable: s as an 8-bit checkpoint (falqon_mx_quantize, E4M3);  bq, b_exp the same of b
  * d is a multiple of 16, at most 16384; 1 <= T <= 2^24, and the launch takes T * d < 2^35 (bf16) or 2^34 (fp32), less for a width between
- * whole waves.
+ * whole waves (scale within fp32).
  */
 typedef struct falqon_norm_fwd_args {
     const void *x, *b, *w, *w_post, *gate;
@@ -529,7 +529,7 @@ falqon_status falqon_token_logprob_bwd_low(const float* d_logp, const void* logi
  *   logp, ref_logp  in  fp32 [T], 0 for tokens that do not count.  A logp of -infinity (a masked label) makes its reward -infinity and the pair's loss
  *             infinite, or without smoothing 0 where it is the rejected one's; a reward without a value (both -infinity) makes the loss NaN
  *   loss, rewards, d_logp  out  fp32 [1], [2, P], [T]
- * 0 <= smoothing < 0.5, beta finite; 1 <= T <= 2^24; 1 <= P <= 65536.  ws: falqon_logprob_workspace_bytes(T, 1, P) bytes.
+ * 0 <= smoothing < 0.5, beta within fp32; 1 <= T <= 2^24; 1 <= P <= 65536.  ws: falqon_logprob_workspace_bytes(T, 1, P) bytes.
  */
 falqon_status falqon_preference_loss(const float* logp, const float* ref_logp, const int64_t* offsets, int64_t T, int64_t P, double beta,
                                      double smoothing, float* loss, float* rewards, float* d_logp, void* ws, size_t ws_bytes, void* stream);

@@ -86,7 +86,7 @@ falqon_status falqon_norm_fwd(const falqon_norm_fwd_args* a, void* stream)
     if (!a) return FALQON_ERR_NULL;
     if (bad_type(a->xt)) return FALQON_ERR_ENUM;
     if (bad_matrix(a->T, a->d, 16) || a->d > kNormMaxWidth || bad_stride(a->ld_x, a->d) || (a->b && bad_stride(a->ld_b, a->d)) ||
-        !std::isfinite(a->scale) || !(a->eps >= 0.0) || norm_fwd_threads(a->T, a->d, a->xt == FALQON_F32) >= int64_t(1) << 32)
+        !std::isfinite(static_cast<float>(a->scale)) || !(a->eps >= 0.0) || norm_fwd_threads(a->T, a->d, a->xt == FALQON_F32) >= int64_t(1) << 32)
         return FALQON_ERR_SHAPE;
     if (!a->x || !a->w || !a->h || !a->rstd || (!a->b && (a->w_post || a->gate || a->bq)) || (a->b && !a->s) || (a->w_post && !a->rstd_b) ||
         !a->sq != !a->s_exp || !a->bq != !a->b_exp)
@@ -109,7 +109,7 @@ falqon_status falqon_norm_bwd(const falqon_norm_bwd_args* a, void* stream)
     if (bad_type(a->xt)) return FALQON_ERR_ENUM;
     const bool codes = a->s_exp != nullptr, reads_b = a->w_post || a->dgate;
     if (bad_matrix(a->T, a->d, 16) || a->d > kNormMaxWidth || bad_stride(a->ld_dh, a->d) || (a->ds && bad_stride(a->ld_ds, a->d)) ||
-        (!codes && (bad_stride(a->ld_s, a->d) || (reads_b && bad_stride(a->ld_b, a->d)))) || !std::isfinite(a->scale))
+        (!codes && (bad_stride(a->ld_s, a->d) || (reads_b && bad_stride(a->ld_b, a->d)))) || !std::isfinite(static_cast<float>(a->scale)))
         return FALQON_ERR_SHAPE;
     if (!a->dh || !a->s || !a->w || !a->rstd || !a->dx || (reads_b && (!a->b || (codes && !a->b_exp))) || (a->w_post && !a->rstd_b) ||
         (a->dw_post && !a->w_post))
@@ -191,7 +191,7 @@ falqon_status falqon_token_logprob_bwd_low(const float* d_logp, const void* logi
 falqon_status falqon_preference_loss(const float* logp, const float* ref_logp, const int64_t* offsets, int64_t T, int64_t P, double beta,
                                      double smoothing, float* loss, float* rewards, float* d_logp, void* ws, size_t ws_bytes, void* stream)
 {
-    if (T < 1 || T > kMaxRows || bad_pairs(P) || !std::isfinite(beta) || !(smoothing >= 0.0 && smoothing < 0.5)) return FALQON_ERR_SHAPE;
+    if (T < 1 || T > kMaxRows || bad_pairs(P) || !std::isfinite(static_cast<float>(beta)) || !(smoothing >= 0.0 && smoothing < 0.5)) return FALQON_ERR_SHAPE;
     if (!logp || !ref_logp || !offsets || !loss || !rewards || !d_logp) return FALQON_ERR_NULL;
     if (any_odd(8, offsets) || any_odd(4, logp, ref_logp, loss, rewards, d_logp) || any_misaligned(ws)) return FALQON_ERR_ALIGN;
     if (!ws || ws_bytes < falqon_logprob_workspace_bytes(T, 1, P)) return FALQON_ERR_WORKSPACE;

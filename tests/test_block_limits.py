@@ -1,13 +1,20 @@
 """Sizes beyond what a launch takes (2^32 - 1 threads along a dimension) are refused as shapes by the operators around the melded layer, before
-anything is launched: nothing is read at these addresses."""
+anything is launched: nothing is read at these addresses.  Numbers of double precision that fp32 does not hold are refused, too."""
 import ctypes as c
 
-from test_block_abi import OK, SHAPE, L, NormFwd  # noqa: F401
+import pytest
+
+from test_block_abi import OK, SHAPE, L, NormBwd, NormFwd  # noqa: F401
 
 
 def norm_fwd(L, **kw):  # noqa: F811
     a = dict(x=OK, b=OK, w=OK, scale=1.0, eps=1e-5, xt=0, T=4, d=64, ld_x=64, ld_b=64, s=OK, h=OK, rstd=OK)
     return L.falqon_norm_fwd(c.byref(NormFwd(**{**a, **kw})), None)
+
+
+def norm_bwd(L, **kw):  # noqa: F811
+    a = dict(dh=OK, ds=OK, s=OK, b=OK, w=OK, rstd=OK, xt=0, T=4, d=64, ld_dh=64, ld_ds=64, ld_s=64, ld_b=64, dx=OK, db=OK, scale=1.0)
+    return L.falqon_norm_bwd(c.byref(NormBwd(**{**a, **kw})), None)
 
 
 def test_passes_over_a_matrix(L):  # noqa: F811
@@ -35,3 +42,9 @@ def test_products(L):  # noqa: F811
     assert f(1 << 24, 32, 1 << 16) == SHAPE                                     # 2^24 tiles of 256 x 256
     assert f(1 << 20, 1 << 15, 64, OK) == SHAPE                                 # the quantizer's pass over x
     assert f(1 << 24, 32, (1 << 16) - 16) == SHAPE                              # a tile more by its last columns
+
+
+@pytest.mark.parametrize("value", [1e39, -1e39, 1e300])
+def test_numbers_beyond_fp32(L, value):  # noqa: F811
+    assert norm_fwd(L, scale=value) == SHAPE and norm_bwd(L, scale=value) == SHAPE
+    assert L.falqon_preference_loss(OK, OK, OK, 4, 2, value, 0.0, OK, OK, OK, OK, 64, None) == SHAPE
