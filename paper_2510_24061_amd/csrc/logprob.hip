@@ -331,8 +331,10 @@ __device__ __forceinline__ double ratio_share(const Preference& a, int64_t from,
     return sum;
 }
 
-// All of it in one workgroup, a wave a sequence.
-constexpr int kOnePairs = 1024;
+// All of it in one workgroup, a wave a sequence: few pairs of few tokens, where a second launch would cost more.  us in one workgroup and in one a pair
+// (those 7.1 to 8.1 throughout): 4 pairs of 16384 tokens in all 5.0, of 32768 6.7, of 65536 10.1 (8.3); 32 pairs of 16384 7.1, of 24000 8.2 (7.8);
+// 48 of 4096 to 16384 7.6 to 8.4, 256 25, 1024 93; one pair of 12000 8.0, of 16384 9.1 (8.1).
+constexpr int kOnePairs = 32, kOneTokens = 16384;
 __global__ void __launch_bounds__(1024)
 preference_one_kernel(const Preference a)
 {
@@ -451,7 +453,7 @@ hipError_t launch_preference_loss(const float* logp, const float* ref, const int
                                   float* loss, float* rewards, float* d_logp, hipStream_t stream)
 {
     const Preference a{logp, ref, offsets, T, static_cast<int>(P), beta, smoothing, loss, rewards, d_logp};
-    if (T <= 16384 && P <= kOnePairs) {
+    if (T <= kOneTokens && P <= kOnePairs) {
         preference_one_kernel<<<1, 1024, 0, stream>>>(a);
     } else {
         preference_pair_kernel<<<static_cast<unsigned>(P), 256, 0, stream>>>(a, pair_loss);

@@ -52,15 +52,15 @@ def launched(f):
 
 
 @pytest.mark.parametrize("smoothing", [0.0, 0.1])
-@pytest.mark.parametrize("T,P", [(16384, 3), (16385, 3), (16385, 1), (50000, 4), (70000, 300), (4000, 1024), (4000, 1025), (20000, 1500), (1, 2000), (300000, 65536)])
+@pytest.mark.parametrize("T,P", [(16384, 3), (16385, 3), (16385, 1), (50000, 4), (70000, 300), (4000, 32), (4000, 33), (4000, 1025), (20000, 1500), (1, 2000), (300000, 65536)])
 def test_a_workgroup_a_pair(T, P, smoothing):
-    """Beyond 16384 tokens or 1024 pairs: a workgroup a pair and one for the mean.  Many pairs have empty sequences among them."""
+    """Beyond 16384 tokens or 32 pairs: a workgroup a pair and one for the mean.  Many pairs have empty sequences among them."""
     g = gen(T + P)
     offsets = torch.sort(torch.randint(T // 9, T - T // 7 + 1, (2 * P + 1,), generator=g))[0]     # tokens before and behind the sequences
     logp, ref = -3 + draw(g, T), -3 + draw(g, T)
     loss_of(logp, offsets, smoothing)
     names = launched(lambda: loss_of(logp, offsets, smoothing))
-    pairs = T > 16384 or P > 1024
+    pairs = T > 16384 or P > 32
     assert ("preference_pair_kernel" in names) == ("preference_mean_kernel" in names) == pairs and ("preference_one_kernel" in names) != pairs
     check_loss(logp, ref, offsets, 0.1, smoothing)
 
