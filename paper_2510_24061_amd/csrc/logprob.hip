@@ -408,7 +408,10 @@ void fwd(const TokenLogprob& a, int splits, hipStream_t stream)
     const int V = static_cast<int>(a.V);
     const dim3 grid(static_cast<unsigned>(a.T), static_cast<unsigned>(splits));
     const auto lse = lse_of<LOW>(a.lse, a.lse_low);
-    token_logprob_kernel<T, LOW><<<grid, a.T < 1024 && a.V >= 8192 ? 1024 : 256, 0, stream>>>(logits, a.ld, V, a.labels, a.logp, lse, a.partial);
+    // Long rows of which there are two a CU at most: 16 waves share one.  us with 256 and with 1024 threads: fp32 512 x 16000 9.3, 7.8, 640 x 16000 10.4, 10.2,
+    // 640 x 32000 15.3, 17.2; bf16 256 x 24000 6.2, 4.9, 512 x 12000 5.0, 5.1, 640 x 12000 5.9, 6.5; 301 x 8192 3.9, 4.5 (bf16) and 3.9, 4.8 (fp32).
+    const int threads = a.T <= 512 && a.V >= 12000 ? 1024 : 256;
+    token_logprob_kernel<T, LOW><<<grid, threads, 0, stream>>>(logits, a.ld, V, a.labels, a.logp, lse, a.partial);
     if (splits > 1)
         token_join_kernel<T, LOW><<<static_cast<unsigned>((a.T + 3) / 4), 256, 0, stream>>>(logits, a.ld, a.T, V, a.labels, a.partial, splits, a.logp, lse);
 }
