@@ -352,7 +352,8 @@ class FusedBlock(torch.nn.Module):
 
 
 class FusedDecoder(torch.nn.Module):
-    """Embedding, blocks, final norm and head: logits of token ids [B, S].  Embedding and head are frozen."""
+    """Embedding, blocks, final norm and head: logits of token ids [B, S].  Embedding and head are frozen.  Whole sequences only: no keys and values are
+    kept, so a one-token step (which the norms and the 4-bit layers have forms for) is that of a model with a cache of its own."""
 
     def __init__(self, embedding: torch.Tensor, head: torch.Tensor, blocks: Sequence[FusedBlock], final: BlockNorm):
         super().__init__()

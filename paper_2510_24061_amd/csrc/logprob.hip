@@ -13,7 +13,7 @@
 // A row is read once forward (running maximum and sum) and once backward; rows that do not count are not read at all.  Vocabularies may
 // be odd, so a row may begin anywhere: the elements up to the first 16-byte boundary and behind the last one are taken one by one.
 // Bound by bytes; the exponentials take about a third of the vector units' time beside them.  In bf16, a third of the tokens not counted:
-// 4096 x 32000 forward 36 us (4.85 TB/s), 8192 x 32000 backward 172 us (5.1 TB/s).
+// 4096 x 32000 forward 36 us (4.85 TB/s), 8192 x 32000 backward 170 to 174 us (5.0 to 5.15 TB/s).
 #include "logprob.h"
 #include "mx_common.h"
 
@@ -178,7 +178,8 @@ token_join_kernel(const T* __restrict__ logits, int64_t ld, int64_t rows, int V,
     if (lane == 0) finish(Running{m, s}, element(logits + t * ld + label), t, logp, lse);
 }
 
-// Sizes of lse from which half of its last place, 2^-18 of a probability and more, is more than the rest of the arithmetic loses.
+// Sizes of lse from which half of its last place, 2^-18 of a probability and more, is more than the rest of the arithmetic loses.  4096 x 32000 in bf16 whose rows
+// are all beyond: 146 us without the low part, 107 with it, which is what rows within take.
 constexpr float kCoarse = 64.0f;
 constexpr int kChunk = 1024;                                          // pieces of a row that a workgroup writes
 

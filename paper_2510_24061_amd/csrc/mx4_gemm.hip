@@ -255,6 +255,8 @@ __device__ __forceinline__ void mx4_tile(const Mx4Gemm& g, int tiles_m, int tile
                 const int i = it * 64 + lane, srw = i / SEGS, seg = i % SEGS;
                 const int64_t row = m0 + wm * (MB * 32) + m * 32 + srw, col = n0 + wn * (NB * 32) + seg * COLS;
                 if (row < g.M && col < g.N) {
+                    // Past the caches at any size: the next reader loses nothing by it.  us of gate and up on one input and the SwiGLU product of them, with
+                    // these stores and with ordinary ones: 64 tokens 4096 -> 11008 22.6, 22.6; 777 70.4, 71.6; 4096 275.5, 274.1; 8192 x 5120 -> 13824 757, 780.
                     typedef unsigned v4u __attribute__((ext_vector_type(4)));
                     __builtin_nontemporal_store(*reinterpret_cast<const v4u*>(part + srw * PITCH + seg * 16), reinterpret_cast<v4u*>(out + (row * g.N + col) * ES));
                 }

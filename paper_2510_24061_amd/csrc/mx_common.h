@@ -128,7 +128,7 @@ __device__ __forceinline__ v4u pack_piece(const float (&f)[4])
     return w;
 }
 
-// Results of a call that are more than the 256 MB memory-side cache holds go past the caches: what reads them next finds them in HBM in either case.
+// Gradients of a call that are more than the 256 MB memory-side cache holds go past the caches: what reads them next finds them in HBM in either case.
 // (A constant of the kernel: of two stores in the branches of an `if` the compiler makes one, an ordinary one.)
 constexpr int64_t kPastCaches = int64_t(256) << 20;
 template <bool PAST>

@@ -12,9 +12,10 @@
 // statistics and weight gradients are fp32.  The backward pass keeps a workgroup on several rows, so that the sums over tokens stay in registers;
 // one partial for each workgroup is left, and a second launch adds them in order (no atomics: the result does not change from run to run).
 // 8192 x 5120 in bf16 with both norms, gate and checkpoints: forward 89 us (4.75 TB/s), backward 84 us (5.05 TB/s, 79 + 5); a copy reaches 5.15.
+// Forward in fp32 (floor): 4096 x 5120 with everything 93 us (74), with a plain branch 68 (66); 8192 x 4096 118 (118) and 99 (105).
 // Rows of more than 8192 columns (fp32: 4096) take two or four pieces a lane in the backward pass and keep the sums over tokens in LDS.
 // With both norms, gate and checkpoints: fp32 4096 x 5120 81 us (floor 73; 111 with the sums in registers, which spill), bf16
-// 4096 x 16384 162 (130; 522).
+// 4096 x 16384 162 (130; 522).  bf16 4096 x 10240 with a plain branch 83 from checkpoints (74), 85 without (82).
 #include "mx_common.h"
 #include "norm.h"
 
@@ -183,8 +184,8 @@ norm_bwd_kernel(const NormBwd a, int waves, int rows_per_group, float* __restric
     constexpr int E = kPiece<T>;
     // One piece a lane: sums and weights stay in registers, and the next row's pieces are on the way.  Two: the sums stand in LDS; in bf16, whose pieces
     // have twice the columns, rows with b are not asked for ahead and their weights come from the caches again for each (otherwise they spill, 4096 x 10240
-    // with both norms 248 us against 112).  Four (fp32 above 8192 columns) are not asked for ahead and spill a little (4096 x 16384 370 us, and 490 with
-    // the weights from the caches).
+    // with both norms 248 us against 112).  What spills all the same: two pieces of bf16 from checkpoints with a plain branch, asked for ahead (5 registers),
+    // and four (fp32 above 8192 columns) with a branch, not asked for ahead (4 to 121; 4096 x 16384 370 us, and 490 with the weights from the caches).
     constexpr bool HELD = P == 1, AHEAD = P * E < 16 || (P == 2 && MODE < 2), KEPT = AHEAD || P == 4;
     __shared__ float slots[2][kMaxWaves];
     extern __shared__ __attribute__((aligned(16))) float gathered[];  // [d] where a workgroup has several rows
