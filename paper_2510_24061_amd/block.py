@@ -33,6 +33,8 @@ def _dense_bf16(t: torch.Tensor, width: int) -> torch.Tensor:
 
 def _check_rows(a, b, what: str) -> None:
     """Leading shapes that name the same rows in the same order: alike up to ones in front, or one of them flat."""
+    if a == b:
+        return
     short, long = sorted((tuple(a), tuple(b)), key=len)
     alike = (1,) * (len(long) - len(short)) + short == long
     if not alike and not (min(len(a), len(b)) <= 1 and torch.Size(a).numel() == torch.Size(b).numel()):
@@ -54,7 +56,8 @@ class _Refused(torch.autograd.Function):
 
 
 def _tie(x: torch.Tensor) -> torch.Tensor:
-    """The last output of a function here, saved last: it holds nothing, and stands for the function in the graph of its gradients."""
+    """The last output of a function here, saved last: it holds nothing, and stands for the function in the graph of its gradients.  (The functions do not have
+    missing gradients made up: there would always be one for it.)"""
     return torch.empty(0, dtype=torch.float32, device=x.device)
 
 
@@ -63,10 +66,10 @@ def _first_order(backward):
     with no graph a penalty on them would be dropped without a word."""
 
     def run(ctx, *grads):
+        if not torch.is_grad_enabled():
+            return backward(ctx, *grads[:-1])
         with torch.no_grad():
             out = backward(ctx, *grads[:-1])
-        if not torch.is_grad_enabled():
-            return out
         again = iter(_Refused.apply(ctx.saved_tensors[-1], *(v.detach() for v in out if isinstance(v, torch.Tensor))))
         return tuple(next(again) if isinstance(v, torch.Tensor) else v for v in out)
 
@@ -144,6 +147,7 @@ class BlockNorm(torch.nn.Module):
 class _SwigluFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, g, u, checkpoint):
+        ctx.set_materialize_grads(False)
         _check_rows(g.shape[:-1], u.shape[:-1], "gate and up")
         g2, u2 = _rows(g), _rows(u)
         T, m = g2.shape
@@ -175,6 +179,7 @@ def swiglu(g: torch.Tensor, u: torch.Tensor, checkpoint: bool = True) -> torch.T
 class _TokenLogprobFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, labels):
+        ctx.set_materialize_grads(False)
         _check_rows(logits.shape[:-1], labels.shape, "logits and labels")
         x = logits.reshape(-1, logits.shape[-1])
         apart = (x.shape[1] == 1 or x.stride(1) == 1) and (x.shape[0] == 1 or x.stride(0) >= x.shape[1])
@@ -204,6 +209,7 @@ def token_logprobs(logits: torch.Tensor, labels: torch.Tensor) -> torch.Tensor:
 class _PreferenceFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logp, ref_logp, offsets, beta, smoothing):
+        ctx.set_materialize_grads(False)
         p2, r2 = logp.reshape(-1).contiguous(), ref_logp.reshape(-1).contiguous()
         T, P, dev = p2.shape[0], (offsets.shape[0] - 1) // 2, logp.device
         loss, rewards, d = (torch.empty(s, dtype=torch.float32, device=dev) for s in (1, (2, P), T))
